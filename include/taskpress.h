@@ -12,6 +12,11 @@
  *                             index set I per KV head (uniform budget, Sec. 4 setup).
  *   4. tp_compact_kv          gather of the kept K rows, quantised V rows and scales
  *                             (the evicted tokens and the guide's KV are dropped).
+ * What follows the path, decoding on the kept tokens in a paged cache of 4-bit keys and values:
+ *   tp_cache_load             the compact cache into pages.
+ *   tp_cache_append           new tokens' keys, rotated at their positions, and values.
+ *   tp_cache_attention        the newest tokens' attention over the pages.
+ *   tp_cache_read             tokens back as bf16 rows, to evict again.
  *
  * Conventions (every entry point):
  *  - Returns tp_status.  All arguments are validated on the host before any GPU
@@ -355,6 +360,153 @@ tp_status tp_evict(const tp_dims* dims, const tp_batch* batch, const void* q_gui
                    float* s_key, float* scales, void* v_q, float* s_out, int32_t* kept_idx,
                    void* k_out, void* v_q_out, float* scales_out, void* workspace, size_t ws_bytes,
                    const tp_profile* profile, void* stream);
+
+/* ------------------------------------------------------------------ the paged 4-bit cache
+ *
+ * Decoding continues on the kept tokens (Sec. 3.1: eviction runs once, after the prefill; Sec. 4
+ * setup: an int4 cache).  A cache holds tokens of many sequences in pages of page_tokens tokens;
+ * row b of the page table lists sequence b's pages in order, so token p of the sequence is token
+ * p % page_tokens of page page_table[b][p / page_tokens].  p counts the tokens held, not positions
+ * of the text: after an eviction a token's rotation position is larger than its place.
+ *
+ * What is held of a token, per (layer, KV head), with codes c in [-7, 7]:
+ *   key    groups of 32 channels, scale = bf16(absmax / 7), c = clamp(RNE(k / scale), -7, 7), all
+ *          codes 0 where the scale is 0, from the bf16 key row (rotated, rounded to bf16 as a
+ *          prefill holds it).  Groups, because channels of keys differ in strength; the scale is
+ *          rounded before the codes are formed, so its rounding is no further error.
+ *   value  Eq. 2 at bits = 4: the scale and codes of tp_quantize_v_scales(TP_QFMT_INT, 4).
+ * The value held is c * scale: 140 bytes a token and head at d = 128 (bf16 rows take 512), 72 at 64.
+ *
+ * pages is one device buffer, bytes [L][num_pages][Hkv][page_tokens / 32][block], where a block
+ * holds 32 tokens of one head in d * 34 + 128 bytes: key codes (16 d bytes), value codes (16 d), key
+ * scales (bf16 [32][d / 32]), value scales (fp32 [32]).  A code is stored as the 4-bit number c + 8,
+ * eight to a little-endian 32-bit word whose nibbles 0..7 hold elements 0, 2, 4, 6, 1, 3, 5, 7:
+ *   keys    [32 tokens][d / 8 words]: word h * (d / 32) + s holds channels 32 s + 8 h + 0..7;
+ *   values  word (x / 64) * 256 + (16 g + x % 16) * 4 + (x / 16) % 4 holds channel x of the tokens
+ *           4 g + 0..3 and 16 + 4 g + 0..3.
+ * These are the operand fragments of the attention's matrix products.  Layer l's part starts at
+ * l * num_pages * Hkv * tp_cache_page_bytes(), so a call for one layer passes that address and L = 1.
+ * Any initial contents are allowed; what a call does not write keeps its value.
+ */
+typedef struct tp_cache {
+  void* pages;               /* device, 16-byte aligned */
+  const int32_t* page_table; /* device [batch][max_pages]; an entry outside [0, num_pages) is no page:
+                                its tokens are not written, not attended to, and read as zeros */
+  const int32_t* lens;       /* device [batch]: tokens held by each sequence, the newest of a step
+                                included; outside [0, max_pages * page_tokens] counts as 0.  Unused (may
+                                be NULL) by tp_cache_load */
+  int64_t num_pages;         /* in [1, 2^31 - 1] */
+  int32_t page_tokens;       /* 32, 64, 128 or 256 */
+  int32_t max_pages;         /* columns of page_table; max_pages * page_tokens <= 2^30 */
+  int32_t batch;             /* sequences, in [1, 65535] */
+} tp_cache;
+
+/* The new tokens of one step.  Sequence b's are rows [offsets[b], offsets[b + 1]) of the step's
+ * tensors and its last ones in the cache: T_b new tokens are tokens lens[b] - T_b .. lens[b] - 1.
+ * A sequence whose range is not within [0, total], decreases, or holds more than max_new tokens
+ * counts as having none (its rows are left as they were), as do rows outside every range. */
+typedef struct tp_step {
+  const int32_t* offsets; /* device [batch + 1], or NULL: row b is sequence b's one token (total >= batch) */
+  int32_t total;          /* rows of the tensors along the token axis, >= 1 */
+  int32_t max_new;        /* most new tokens of a sequence, >= 1 (1 when offsets is NULL) */
+} tp_step;
+
+/* bf16 rows [L][total][heads][d] at any strides (in elements, multiples of 8, >= 0; d contiguous),
+ * 16-byte aligned: both [tokens][heads][d] slices of a projection's output and head-major tensors.
+ * An output's rows may not overlap. */
+typedef struct tp_rows {
+  void* data;
+  int64_t layer_stride, token_stride, head_stride;
+} tp_rows;
+
+/* Rotation of query and key rows by their positions: in the first rotary_dim channels, pair
+ * (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin) with the pair's entry of the position's row. */
+enum {
+  TP_ROPE_HALVES = 0, /* pair i is channels (i, i + rotary_dim / 2) */
+  TP_ROPE_PAIRS = 1   /* pair i is channels (2 i, 2 i + 1) */
+};
+typedef struct tp_rope {
+  const float* cos_sin;  /* device fp32 [num_positions][rotary_dim]: rotary_dim / 2 cosines, then the
+                            sines; 16-byte aligned */
+  int64_t num_positions; /* >= 1 */
+  int32_t rotary_dim;    /* a multiple of 16 in [16, head_dim] */
+  int32_t style;         /* TP_ROPE_* */
+} tp_rope;
+
+/* Bytes of one page of one (layer, KV head): page_tokens * (d + d / 16 + 4); 0 for arguments that no
+ * cache has (tp_last_error() says which).  Host only. */
+size_t tp_cache_page_bytes(const tp_dims* dims, int32_t page_tokens);
+
+/*
+ * The compact cache of an eviction (tp_evict, tp_compact_kv, tp_compact_quantize_kv with TP_QFMT_INT
+ * and bits <= 4) into the pages, as the first tokens of its sequences: for t < k_b = kept_offsets[b + 1] -
+ * kept_offsets[b], token t of sequence b gets the key k[l][h][kept_offsets[b] + t] (quantised as above) and
+ * the codes and scale v_q, scales of that row, copied.
+ * kept_offsets: host [batch + 1] from 0, nondecreasing, k_b <= max_pages * page_tokens (TP_ERR_SHAPE);
+ * k bf16 [L][Hkv][K_tot][d], v_q bytes [L][Hkv][K_tot][d / 2], scales fp32 [L][Hkv][K_tot], contiguous,
+ * 16-byte aligned.  cache->batch <= TP_MAX_BATCH.  bits in [2, 4], the bits v_q was quantised with.
+ * The keys are finite.  lens is neither read nor set.
+ * Errors: TP_ERR_NULL, TP_ERR_SHAPE, TP_ERR_PARAM, TP_ERR_UNSUPPORTED, TP_ERR_HIP.
+ */
+tp_status tp_cache_load(const tp_dims* dims, const tp_cache* cache, const int64_t* kept_offsets, const void* k,
+                        const void* v_q, const float* scales, int32_t bits, void* stream);
+
+/*
+ * A step's new tokens into the pages, their keys rotated on the way; with q, their query rows rotated
+ * beside them, so one call prepares a layer's attention.
+ *   key   token t of sequence b is written from k's row offsets[b] + t, rotated at positions[row];
+ *   value from v's row;
+ *   q_out[row] = q[row] rotated, for every row of a sequence; q_out may be q (the same data and strides).
+ * The rotation's products and sums are formed in 64 bits and rounded to bf16 once (nearest even; beyond the
+ * largest finite value to that value); the key's codes are formed from the rounded row.
+ * positions: device int32 [total]; a row whose position is outside [0, num_positions) is not written
+ * (neither key, value nor q_out).  rope NULL: no rotation, positions unused (may be NULL), q and
+ * q_out NULL.  q and q_out are given together.
+ * k, v rows of Hkv heads, q, q_out of Hq.  New tokens that lie before the sequence's start
+ * (lens[b] < T_b) are not written.  A page that two sequences share may be written by neither.
+ * Inputs are finite.
+ * Errors: TP_ERR_NULL, TP_ERR_SHAPE, TP_ERR_PARAM, TP_ERR_UNSUPPORTED, TP_ERR_HIP.
+ */
+tp_status tp_cache_append(const tp_dims* dims, const tp_cache* cache, const tp_step* step, const tp_rows* k,
+                          const tp_rows* v, const int32_t* positions, const tp_rope* rope, const tp_rows* q,
+                          const tp_rows* q_out, void* stream);
+
+/* Bytes of workspace tp_cache_attention needs for these arguments (host only; may be 0).  Never falls
+ * when total, max_new, max_len or the batch grows. */
+tp_status tp_cache_workspace_size(const tp_dims* dims, const tp_cache* cache, const tp_step* step, int64_t max_len,
+                                  size_t* bytes);
+
+/*
+ * Attention of a step's tokens over the cache (their own keys and values included: append first).
+ * New token t of sequence b attends to its tokens 0 .. lens[b] - T_b + t:
+ *   x_p = softmax_scale * <q[row], key_p>,   o[row] = sum_p exp(x_p) value_p / sum_p exp(x_p),
+ *   lse[l][r][row] = ln sum_p exp(x_p)
+ * for every query head r of KV head r / (Hq / Hkv).  A row that attends to nothing (an empty
+ * sequence, t < T_b - lens[b], pages missing throughout) gets o = 0 and lse = -infinity.
+ * q, o rows of Hq heads; o is rounded to bf16 once; lse fp32 [L][Hq][total], 4-byte aligned, or NULL.
+ * max_len: at least every lens[b] (host; in [1, max_pages * page_tokens]); a longer sequence counts
+ * as empty.  softmax_scale > 0, finite.
+ * workspace: device, >= tp_cache_workspace_size() bytes, 256-byte aligned (NULL if that is 0).
+ * Maxima, sums and outputs are held in fp32; the weights times the values' scales are rounded to fp16
+ * (relative to the row's largest) for the value product.
+ * Errors: TP_ERR_NULL, TP_ERR_SHAPE, TP_ERR_PARAM, TP_ERR_UNSUPPORTED, TP_ERR_WORKSPACE, TP_ERR_HIP.
+ */
+tp_status tp_cache_attention(const tp_dims* dims, const tp_cache* cache, const tp_step* step, const tp_rows* q,
+                             float softmax_scale, int64_t max_len, const tp_rows* o, float* lse, void* workspace,
+                             size_t ws_bytes, void* stream);
+
+/*
+ * Ranges of the sequences back as bf16 rows, the layout the eviction takes (a long answer is evicted
+ * again): for t < n_b = ctx_offsets[b + 1] - ctx_offsets[b] and p = first[b] + t,
+ *   k_out[l][h][ctx_offsets[b] + t][:] = bf16(key held of token p),  v_out likewise,
+ * zero rows for p >= lens[b] and for tokens without a page.  batch->batch = cache->batch (so at most
+ * TP_MAX_BATCH); ctx_offsets as tp_batch, but a range may be empty; guide_offsets unused.  first: host
+ * [batch], >= 0, first[b] + n_b <= 2^30 (TP_ERR_SHAPE); NULL: 0.  k_out, v_out bf16 [L][Hkv][N_tot][d],
+ * 16-byte aligned.
+ * Errors: TP_ERR_NULL, TP_ERR_SHAPE, TP_ERR_PARAM, TP_ERR_UNSUPPORTED, TP_ERR_HIP.
+ */
+tp_status tp_cache_read(const tp_dims* dims, const tp_cache* cache, const tp_batch* batch, const int64_t* first,
+                        void* k_out, void* v_out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -25,8 +25,11 @@ EXPORTED = ("tp_version", "tp_status_string", "tp_last_error", "tp_keep_count", 
             "tp_guide_scores", "tp_guide_scores_lse", "tp_guide_attention", "tp_guide_attention_quantize",
             "tp_quantize_v_scales",
             "tp_combine_select_topk",
-            "tp_combine_select_topk_static", "tp_compact_kv", "tp_compact_quantize_kv", "tp_evict")
+            "tp_combine_select_topk_static", "tp_compact_kv", "tp_compact_quantize_kv", "tp_evict",
+            "tp_cache_page_bytes", "tp_cache_load", "tp_cache_append", "tp_cache_workspace_size",
+            "tp_cache_attention", "tp_cache_read")
 TP_STATIC_SCRATCH_BYTES = 64 << 20
+TP_ROPE_HALVES, TP_ROPE_PAIRS = 0, 1
 
 
 class TaskPressError(RuntimeError):
@@ -51,6 +54,26 @@ class TpBatch(ctypes.Structure):
 
 class TpProfile(ctypes.Structure):
     _fields_ = [("num_events", ctypes.c_int32), ("events", ctypes.c_void_p * TP_EVICT_EVENTS)]
+
+
+class TpCache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("batch", ctypes.c_int32)]
+
+
+class TpStep(ctypes.Structure):
+    _fields_ = [("offsets", ctypes.c_void_p), ("total", ctypes.c_int32), ("max_new", ctypes.c_int32)]
+
+
+class TpRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class TpRope(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("num_positions", ctypes.c_int64), ("rotary_dim", ctypes.c_int32),
+                ("style", ctypes.c_int32)]
 
 
 def _i64_array(vals):
@@ -135,6 +158,19 @@ def load():
     lib.tp_evict.argtypes = [pd, pb, P, P, P, P, P, ctypes.c_float, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                              ctypes.c_int32, ctypes.c_double, ctypes.c_int64, pi64, P, P, P, P, P, P, P, P, P,
                              ctypes.c_size_t, ctypes.POINTER(TpProfile), P]
+    pc, ps, pr = ctypes.POINTER(TpCache), ctypes.POINTER(TpStep), ctypes.POINTER(TpRows)
+    lib.tp_cache_page_bytes.restype = ctypes.c_size_t
+    lib.tp_cache_page_bytes.argtypes = [pd, ctypes.c_int32]
+    lib.tp_cache_load.restype = ctypes.c_int32
+    lib.tp_cache_load.argtypes = [pd, pc, pi64, P, P, P, ctypes.c_int32, P]
+    lib.tp_cache_append.restype = ctypes.c_int32
+    lib.tp_cache_append.argtypes = [pd, pc, ps, pr, pr, P, ctypes.POINTER(TpRope), pr, pr, P]
+    lib.tp_cache_workspace_size.restype = ctypes.c_int32
+    lib.tp_cache_workspace_size.argtypes = [pd, pc, ps, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)]
+    lib.tp_cache_attention.restype = ctypes.c_int32
+    lib.tp_cache_attention.argtypes = [pd, pc, ps, pr, ctypes.c_float, ctypes.c_int64, pr, P, P, ctypes.c_size_t, P]
+    lib.tp_cache_read.restype = ctypes.c_int32
+    lib.tp_cache_read.argtypes = [pd, pc, pb, pi64, P, P, P]
     _lib = lib
     return lib
 
@@ -436,3 +472,171 @@ def evict_fused(d: TpDims, batch: Batch, q_guide, k, v, *, softmax_scale: float,
              bufs.s_key, bufs.scales, bufs.v_q if full_codes else None, bufs.s_comb, bufs.kept_idx, bufs.k_c,
              bufs.v_q_c, bufs.scales_c, bufs.ws_evict, events, stream, k_guide, guide_lse)
     return bufs
+
+
+# ----------------------------------------------------------------------------- the paged 4-bit cache
+def _device_tensor(t, dtype, name, shape=None):
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor of {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    return t
+
+
+class Cache:
+    """A tp_cache and the tensors it points to (kept alive here): `pages` uint8 of
+    L * num_pages * Hkv * tp_cache_page_bytes(d, page_tokens) bytes, `page_table` int32 [batch][max_pages],
+    `lens` int32 [batch] (None for a cache that is only loaded).  All calls on one handle see what the
+    tensors hold when the work runs, so lengths and table are updated in place from step to step."""
+
+    def __init__(self, d: TpDims, pages, page_table, lens, page_tokens: int):
+        each = tp_cache_page_bytes(d, page_tokens) * d.num_layers * d.num_kv_heads
+        if not pages.is_cuda or not pages.is_contiguous():
+            raise ValueError("pages must be a contiguous device tensor")
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [batch][max_pages]")
+        _device_tensor(page_table, torch.int32, "page_table")
+        if lens is not None:
+            _device_tensor(lens, torch.int32, "lens", page_table.shape[:1])
+        if page_table.device != pages.device or (lens is not None and lens.device != pages.device):
+            raise ValueError("pages, page_table and lens must be on one device")
+        if _nbytes(pages) == 0 or _nbytes(pages) % each:
+            raise ValueError(f"pages holds {_nbytes(pages)} bytes, needs a multiple of {each}")
+        self.pages, self.page_table, self.lens, self.device = pages, page_table, lens, pages.device
+        self.dims = (d.num_layers, d.num_q_heads, d.num_kv_heads, d.head_dim)
+        self.batch, self.page_tokens = page_table.shape[0], int(page_tokens)
+        self.c = TpCache(pages.data_ptr(), page_table.data_ptr(), None if lens is None else lens.data_ptr(),
+                         _nbytes(pages) // each, int(page_tokens), page_table.shape[1], page_table.shape[0])
+        self.ref = ctypes.byref(self.c)
+
+
+class Step:
+    """A tp_step: `total` rows along the token axis, at most `max_new` new tokens of a sequence, `offsets`
+    int32 [batch + 1] on the device (None: row b is sequence b's one token)."""
+
+    def __init__(self, total: int, max_new: int = 1, offsets=None):
+        if offsets is not None:
+            _device_tensor(offsets, torch.int32, "offsets")
+        self.offsets, self.total, self.max_new = offsets, int(total), int(max_new)
+        self.c = TpStep(None if offsets is None else offsets.data_ptr(), self.total, self.max_new)
+        self.ref = ctypes.byref(self.c)
+
+
+class Rope:
+    """A tp_rope: `cos_sin` fp32 [num_positions][rotary_dim], rotary_dim / 2 cosines, then the sines."""
+
+    def __init__(self, cos_sin, rotary_dim: int, style: int = TP_ROPE_HALVES):
+        _device_tensor(cos_sin, torch.float32, "cos_sin")
+        if cos_sin.dim() != 2 or cos_sin.shape[1] != rotary_dim:
+            raise ValueError(f"cos_sin has shape {tuple(cos_sin.shape)}, needs [positions][{rotary_dim}]")
+        self.cos_sin = cos_sin
+        self.c = TpRope(cos_sin.data_ptr(), cos_sin.shape[0], int(rotary_dim), int(style))
+        self.ref = ctypes.byref(self.c)
+
+
+def _rows(t, d: TpDims, heads: int, step: Step, name: str):
+    """tp_rows of a bf16 tensor [total][heads][d] (one layer) or [L][total][heads][d] at any strides; a
+    head-major tensor is given as its permuted view."""
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be a device tensor of torch.bfloat16")
+    shape, strides = tuple(t.shape), t.stride()
+    if len(shape) == 3:
+        shape, strides = (1, *shape), (0, *strides)
+    if shape != (d.num_layers, step.total, heads, d.head_dim):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, needs "
+                         f"{(d.num_layers, step.total, heads, d.head_dim)} ([L][total][heads][d])")
+    if strides[3] != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return TpRows(t.data_ptr(), *strides[:3])
+
+
+def _cache_call(d: TpDims, cache: Cache, tensors, stream):
+    """The stream of a call (the current one of the cache's device), after the checks all calls share."""
+    if (d.num_layers, d.num_q_heads, d.num_kv_heads, d.head_dim) != cache.dims:
+        raise ValueError("the cache was made for other dims")
+    for t in tensors:
+        if t is not None and t.device != cache.device:
+            raise ValueError(f"a tensor on {t.device} for a cache on {cache.device}")
+    if stream is None:
+        return torch.cuda.current_stream(cache.device).cuda_stream
+    return _stream(stream)
+
+
+def _need_step(cache: Cache, step: Step):
+    if step.offsets is not None and step.offsets.numel() != cache.batch + 1:
+        raise ValueError(f"offsets holds {step.offsets.numel()} entries, needs {cache.batch + 1}")
+
+
+def tp_cache_page_bytes(d: TpDims, page_tokens: int) -> int:
+    n = int(load().tp_cache_page_bytes(ctypes.byref(d), int(page_tokens)))
+    if n == 0:
+        raise TaskPressError(TP_ERR_UNSUPPORTED, load().tp_last_error().decode())
+    return n
+
+
+def tp_cache_load(d: TpDims, cache: Cache, kept_offsets, k, v_q, scales, bits: int, stream=None):
+    """The compact cache (k bf16 [L][Hkv][K_tot][d], v_q [L][Hkv][K_tot][d / 2], scales [L][Hkv][K_tot])
+    into the pages, as the first tokens of the cache's sequences."""
+    s = _cache_call(d, cache, (k, v_q, scales), stream)
+    n = d.num_layers * d.num_kv_heads * int(kept_offsets[-1])
+    if len(kept_offsets) != cache.batch + 1:
+        raise ValueError(f"kept_offsets holds {len(kept_offsets)} entries, needs {cache.batch + 1}")
+    _need(k, n * d.head_dim * 2, "k")
+    _need(v_q, n * d.head_dim // 2, "v_q")
+    _need(scales, n * 4, "scales")
+    _check(load().tp_cache_load(ctypes.byref(d), cache.ref, _i64_array(kept_offsets), _ptr(k), _ptr(v_q),
+                                _ptr(scales), int(bits), s))
+
+
+def tp_cache_append(d: TpDims, cache: Cache, step: Step, k, v, positions=None, rope: Rope = None, q=None, q_out=None,
+                    stream=None):
+    """A step's keys (rotated at `positions` int32 [total]) and values into the pages, and q's rows rotated
+    into q_out.  k, v [total][Hkv][d], q, q_out [total][Hq][d] (or with a leading [L]), any strides."""
+    s = _cache_call(d, cache, (k, v, positions, q, q_out, step.offsets, None if rope is None else rope.cos_sin), stream)
+    _need_step(cache, step)
+    rk, rv = _rows(k, d, d.num_kv_heads, step, "k"), _rows(v, d, d.num_kv_heads, step, "v")
+    rq = ro = None
+    if q is not None:
+        rq = ctypes.byref(_rows(q, d, d.num_q_heads, step, "q"))
+    if q_out is not None:
+        ro = ctypes.byref(_rows(q_out, d, d.num_q_heads, step, "q_out"))
+    if positions is not None:
+        _device_tensor(positions, torch.int32, "positions", (step.total,))
+    _check(load().tp_cache_append(ctypes.byref(d), cache.ref, step.ref, ctypes.byref(rk), ctypes.byref(rv),
+                                  _ptr(positions), None if rope is None else rope.ref, rq, ro, s))
+
+
+def tp_cache_workspace_size(d: TpDims, cache: Cache, step: Step, max_len: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().tp_cache_workspace_size(ctypes.byref(d), cache.ref, step.ref, int(max_len), ctypes.byref(out)))
+    return int(out.value)
+
+
+def tp_cache_attention(d: TpDims, cache: Cache, step: Step, q, softmax_scale: float, max_len: int, o, lse=None,
+                       workspace=None, stream=None):
+    """Attention of a step's rows q [total][Hq][d] over the cache: o likewise (bf16), lse fp32 [L][Hq][total]
+    (natural log) or None."""
+    s = _cache_call(d, cache, (q, o, lse, workspace, step.offsets), stream)
+    _need_step(cache, step)
+    rq, ro = _rows(q, d, d.num_q_heads, step, "q"), _rows(o, d, d.num_q_heads, step, "o")
+    if lse is not None:
+        _need(lse, d.num_layers * d.num_q_heads * step.total * 4, "lse")
+    if workspace is None:
+        workspace = torch.empty(tp_cache_workspace_size(d, cache, step, max_len), dtype=torch.uint8, device=cache.device)
+        if stream is not None:  # allocated on the current stream: kept until the work on the other one is done
+            workspace.record_stream(torch.cuda.ExternalStream(s, device=cache.device))
+    _check(load().tp_cache_attention(ctypes.byref(d), cache.ref, step.ref, ctypes.byref(rq), float(softmax_scale),
+                                     int(max_len), ctypes.byref(ro), _ptr(lse), _ptr(workspace), _nbytes(workspace), s))
+
+
+def tp_cache_read(d: TpDims, cache: Cache, batch: Batch, k_out, v_out, first=None, stream=None):
+    """Tokens first[b] .. first[b] + n_b - 1 of each sequence (n_b from batch.ctx_offsets) as bf16 rows
+    [L][Hkv][N_tot][d]."""
+    s = _cache_call(d, cache, (k_out, v_out), stream)
+    n = d.num_layers * d.num_kv_heads * batch.n_tot * d.head_dim * 2
+    _need(k_out, n, "k_out")
+    _need(v_out, n, "v_out")
+    if first is not None and len(first) != cache.batch:
+        raise ValueError(f"first holds {len(first)} entries, needs {cache.batch}")
+    _check(load().tp_cache_read(ctypes.byref(d), cache.ref, ctypes.byref(batch.c),
+                                None if first is None else _i64_array(first), _ptr(k_out), _ptr(v_out), s))

@@ -9,11 +9,16 @@
 #include <mutex>
 #include <string>
 
+#include "abi_internal.h"
 #include "tp_internal.h"
 
+// Shared with abi_cache.cpp (abi_internal.h).
+namespace tp {
 namespace {
 
 thread_local std::string g_err;
+
+}  // namespace
 
 tp_status fail(tp_status s, const char* fmt, ...) {
   char buf[512];
@@ -56,6 +61,21 @@ tp_status check_offsets(const int64_t* off, int32_t batch, const char* what, boo
                   (long long)off[b + 1]);
   return TP_OK;
 }
+
+tp_status hip_fail(hipError_t e, const char* where) {
+  return fail(TP_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
+}
+
+}  // namespace tp
+
+namespace {
+
+using tp::aligned16;
+using tp::check_dims;
+using tp::check_offsets;
+using tp::fail;
+using tp::hip_fail;
+using tp::ok;
 
 // The batch's offsets (nondecreasing from 0, each sequence non-empty), and extents for which
 // every size the layouts derive fits in 64 bits and every launch fits its grid (a dispatch
@@ -103,10 +123,6 @@ tp::BatchArgs batch_args(const tp_batch* bt, bool with_guides) {
     a.g_off[b] = with_guides ? bt->guide_offsets[b] : 0;
   }
   return a;
-}
-
-tp_status hip_fail(hipError_t e, const char* where) {
-  return fail(TP_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
 }
 
 size_t select_workspace(const tp_dims* d, const tp_batch* bt) {
@@ -453,7 +469,7 @@ const char* tp_status_string(tp_status s) {
   }
 }
 
-const char* tp_last_error(void) { return g_err.c_str(); }
+const char* tp_last_error(void) { return tp::g_err.c_str(); }
 
 int64_t tp_keep_count(int64_t n, double keep_ratio, int64_t keep_budget) {
   if (n < 1) return -1;
