@@ -29,6 +29,9 @@ namespace {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kAttnThreads = 256;
@@ -43,6 +46,10 @@ constexpr float kSet = 8.0f, kLimit = 16384.0f;
 // with tiny or zero values cannot overflow the sum.
 constexpr float kLeastScale = 0x1p-60f;
 
+// Key scales as fp16 numbers: the largest of a block is set to exponent field 24 (2^9), and the setting is kept
+// while the largest of a block has field 14 to 27 (a code times a scale stays below 2^16).
+constexpr int kScaleSet = 24, kScaleLow = 14 << 7, kScaleHigh = 28 << 7;
+
 union Frag {
   uint32_t w[4];
   f16x8 h;
@@ -56,16 +63,20 @@ __device__ inline uint32_t pack_h(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, two);
 }
 
-// Eight codes as fp16 numbers c.
-__device__ inline Frag codes(uint32_t w) {
+__device__ inline u16x2 pair(uint32_t w) { return __builtin_bit_cast(u16x2, w); }
+__device__ inline u16x2 max_pair(u16x2 a, u16x2 b) { return __builtin_elementwise_max(a, b); }
+
+// Eight codes as fp16 numbers c.  magic: 0x64006400 in a vector register (with both constants scalar, the
+// and and the or cannot be one instruction).
+__device__ inline Frag codes(uint32_t w, uint32_t magic) {
   Frag f;
   const f16x2 low = {(_Float16)-1032.0f, (_Float16)-1032.0f}, high = {(_Float16)-72.0f, (_Float16)-72.0f};
   const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
 #pragma unroll
   for (int i = 0; i < 4; i += 2) {
     const uint32_t x = w >> (4 * i);
-    const f16x2 a = __builtin_bit_cast(f16x2, (x & 0x000F000Fu) | 0x64006400u) + low;  // 1024 + u
-    const f16x2 b = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (x & 0x00F000F0u) | 0x64006400u), sixteenth,
+    const f16x2 a = __builtin_bit_cast(f16x2, (x & 0x000F000Fu) | magic) + low;  // 1024 + u
+    const f16x2 b = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (x & 0x00F000F0u) | magic), sixteenth,
                                               high);  // 1024 + 16 u
     f.w[i] = __builtin_bit_cast(uint32_t, a);
     f.w[i + 1] = __builtin_bit_cast(uint32_t, b);
@@ -77,20 +88,19 @@ __device__ inline Frag codes(uint32_t w) {
 struct RowGroup {
   int row0, rows;      // the group's first row, and the sequence's rows
   int before;          // tokens before the step's (negative: the sequence holds fewer than the step)
-  int keys, active;    // keys of the group's last row; chunks with any (at least 1)
+  int keys;            // keys of the group's last row: chunk c has some where c * chunk < keys
 };
 __device__ inline RowGroup row_group(const CacheAttnArgs& a, const StepSeq& q, int group, int width) {
   RowGroup r;
   r.row0 = group * width;
-  r.rows = q.count * a.R;
+  r.rows = q.count * (int)a.R.d;
   r.before = q.len - q.count;
-  r.keys = max(0, r.before + (min(r.rows, r.row0 + width) - 1) / a.R + 1);
-  r.active = max(1, (r.keys + a.chunk - 1) / a.chunk);
+  r.keys = __builtin_amdgcn_readfirstlane(max(0, r.before + a.R.div(max(min(r.rows, r.row0 + width) - 1, 0)) + 1));
   return r;
 }
 
 template <int D, int NR>
-__global__ __launch_bounds__(kAttnThreads) void k_cache_attention(CacheAttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k_cache_attention(CacheAttnArgs a) {
   using B = CacheBlock<D>;
   constexpr int KS = D / 32;  // products of a score: channels in steps of 32
   constexpr int ND = D / 16;  // output tiles: channels in steps of 16
@@ -98,27 +108,31 @@ __global__ __launch_bounds__(kAttnThreads) void k_cache_attention(CacheAttnArgs 
   __shared__ float lds_o[kAttnWaves][16][kStride];
   __shared__ float2 lds_stat[kAttnWaves][16 * NR];
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15;
-  const int heads = a.c.L * a.c.Hkv;
-  const int lh = (int)blockIdx.x % heads, rest = (int)blockIdx.x / heads;
-  const int layer = lh / a.c.Hkv, head = lh % a.c.Hkv;
-  const int group = rest % a.row_groups, chunk = rest / a.row_groups;
+  const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest);
+  const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
+  const int chunk = a.by_groups.div(rest), group = a.by_groups.mod(rest, chunk);
   const int b = blockIdx.y;
+  // the chunk's pages, one a lane (a chunk has at most 64)
+  const int page0 = (chunk * a.chunk / kCacheBlock) >> a.c.page_shift;
+  int pages = page0 + lane < a.c.max_pages ? a.c.table[(int64_t)b * a.c.max_pages + page0 + lane] : -1;
   const StepSeq q = step_sequence(a.c, a.s, b);
   const RowGroup rg = row_group(a, q, group, 16 * NR);
-  if (rg.row0 >= rg.rows || chunk >= rg.active) return;
+  if (rg.row0 >= rg.rows || (chunk > 0 && chunk * a.chunk >= rg.keys)) return;
+  if (pages >= a.c.num_pages) pages = -1;
 
   Frag qf[NR][KS];
-  float scale[NR];  // softmax_scale * log2(e), and the power of two that the row was divided by
+  int shift[NR];    // the power of two that the row was multiplied by
+  float scale[NR];  // softmax_scale * log2(e), less that power and the key scales'
   int seen[NR];     // keys of the lane's row
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     const int row = rg.row0 + r * 16 + n;
-    const int t = row / a.R;
+    const int t = a.R.div(row);
     const bool in = row < rg.rows;
     seen[r] = in ? rg.before + t + 1 : 0;
-    const uint16_t* p = a.q.data + layer * a.q.layer + (q.row + t) * a.q.token + (head * a.R + row % a.R) * a.q.head;
+    const uint16_t* p = a.q.data + layer * a.q.layer + (q.row + t) * a.q.token + (head * (int)a.R.d + a.R.mod(row, t)) * a.q.head;
     uint4 x[KS];
     uint32_t top = 0;  // the row's largest magnitude, as bf16 bits
 #pragma unroll
@@ -131,7 +145,8 @@ __global__ __launch_bounds__(kAttnThreads) void k_cache_attention(CacheAttnArgs 
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
     const int e = 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(top << 16));  // the largest comes to [2^14, 2^15)
-    scale[r] = __builtin_amdgcn_ldexpf(a.scale_log2, -e);
+    shift[r] = e;
+    scale[r] = __builtin_amdgcn_ldexpf(a.scale_log2, -112 - e);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const uint32_t w[4] = {x[s].x, x[s].y, x[s].z, x[s].w};
@@ -141,6 +156,9 @@ __global__ __launch_bounds__(kAttnThreads) void k_cache_attention(CacheAttnArgs 
                                __builtin_amdgcn_ldexpf(__uint_as_float(w[i] & 0xFFFF0000u), e));
     }
   }
+
+  uint32_t magic = 0x64006400u;
+  asm("" : "+v"(magic));
 
   f32x4 acc[NR][ND];
   float m[NR], l[NR];
@@ -153,74 +171,106 @@ __global__ __launch_bounds__(kAttnThreads) void k_cache_attention(CacheAttnArgs 
   }
 
   const int key0 = chunk * a.chunk, key1 = min(rg.keys, key0 + a.chunk);
-  const int blocks = (key1 - key0 + kCacheBlock - 1) / kCacheBlock;
-  const int per = (blocks + kAttnWaves - 1) / kAttnWaves;
-  const int j0 = key0 / kCacheBlock + wave * per;
-  const int j1 = min(j0 + per, key0 / kCacheBlock + blocks);
-  const int all_seen = rg.before + rg.row0 / a.R + 1;  // keys before this one are seen by every row of the group
-  // the wave's pages, one a lane: a chunk of 8192 tokens gives a wave 64 blocks, so at most 64 pages
-  const int page0 = j0 >> a.c.page_shift;
-  int pages = -1;
-  if (j0 < j1 && page0 + lane < a.c.max_pages) {
-    pages = a.c.table[(int64_t)b * a.c.max_pages + page0 + lane];
-    if (pages >= a.c.num_pages) pages = -1;
-  }
+  const int j0 = key0 / kCacheBlock + wave, j1 = (key1 + kCacheBlock - 1) / kCacheBlock;  // every fourth block
+  const int all_seen = rg.before + a.R.div(rg.row0) + 1;  // keys before this one are seen by every row of the group
 
-  for (int j = j0; j < j1; ++j) {
-    const int page = __builtin_amdgcn_readlane(pages, (j >> a.c.page_shift) - page0);
-    if (page < 0) continue;
+  // Block j's part of the lane, in registers: keys' words and scales, values' words and scales.
+  u32x4 kw[2], vw[ND / 4], vs[2];
+  u32x2 ks[2];
+  const auto page_of = [&](int j) { return __builtin_amdgcn_readlane(pages, (j >> a.c.page_shift) - page0); };
+  const auto block_at = [&](int j) {
+    const int page = max(page_of(j), 0);  // a missing page: any
     const int64_t at = (((int64_t)layer * a.c.num_pages + page) * a.c.Hkv + head) << a.c.page_shift;
-    const uint8_t* blk = a.c.pages + (at + (j & ((1 << a.c.page_shift) - 1))) * B::kBytes;
-    uint32_t kw[2][KS], vw[ND];
-    float ks[2][4][KS], vs[8];
+    uint8_t* blk = a.c.pages + (at + (j & ((1 << a.c.page_shift) - 1))) * B::kBytes;
+    return __builtin_amdgcn_make_buffer_rsrc(blk, 0, B::kBytes, 0x00020000);
+  };
+  // the lane's places in a block
+  const int at_key = n * (D / 2) + g * KS * 4, at_key_scale = n * KS * 2;
+  const int at_value = lane * 16, at_value_scale = g * 16;
+  const auto load_keys = [&](__amdgpu_buffer_rsrc_t blk) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const uint32_t* kp = (const uint32_t*)(blk + B::kKeys) + (u * 16 + n) * (D / 8) + g * KS;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) kw[u][s] = kp[s];
-      const uint16_t* sp = (const uint16_t*)(blk + B::kKeyScales) + (u * 16 + g * 4) * KS;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int s = 0; s < KS; s += 2) {
-          const uint32_t w = *(const uint32_t*)(sp + i * KS + s);
-          ks[u][i][s] = __uint_as_float(w << 16);
-          ks[u][i][s + 1] = __uint_as_float(w & 0xFFFF0000u);
-        }
-      const float4 v = *(const float4*)((const float*)(blk + B::kValueScales) + u * 16 + g * 4);
-      vs[u * 4] = v.x;
-      vs[u * 4 + 1] = v.y;
-      vs[u * 4 + 2] = v.z;
-      vs[u * 4 + 3] = v.w;
+      if (KS == 4) {
+        kw[u] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_key, B::kKeys + u * 8 * D, 0);
+        ks[u] = __builtin_amdgcn_raw_buffer_load_b64(blk, at_key_scale, B::kKeyScales + u * D, 0);
+      } else {
+        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(blk, at_key, B::kKeys + u * 8 * D, 0);
+        kw[u] = (u32x4){w.x, w.y, 0, 0};
+        ks[u] = (u32x2){__builtin_amdgcn_raw_buffer_load_b32(blk, at_key_scale, B::kKeyScales + u * D, 0), 0};
+      }
     }
+  };
+  const auto load_values = [&](__amdgpu_buffer_rsrc_t blk) {
 #pragma unroll
-    for (int x = 0; x < ND; ++x) vw[x] = *((const uint32_t*)(blk + B::kValues) + (x >> 2) * 256 + lane * 4 + (x & 3));
+    for (int x = 0; x < ND / 4; ++x) vw[x] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_value, B::kValues + x * 1024, 0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) vs[u] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_value_scale, B::kValueScales + u * 64, 0);
+  };
+  if (j0 < j1) {
+    const auto blk = block_at(j0);
+    load_keys(blk);
+    load_values(blk);
+  }
+  int bias = 0;  // bf16 bits taken off a key scale: it becomes an fp16 number times 2^(bias / 128 - 112)
+  for (int j = j0; j < j1; j += kAttnWaves) {
+    const bool missing = page_of(j) < 0;
+    const bool masked = missing || (j + 1) * kCacheBlock > all_seen;
+    if (masked) {  // scales of slots that no row sees may be anything
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (missing || j * kCacheBlock + u * 16 + n >= rg.keys) ks[u] = (u32x2){0, 0};
+    }
+    // Key scales to fp16: bf16 bits, with the exponent brought into range and the mantissa moved by 3 bits.
+    const u16x2 top2 = max_pair(max_pair(pair(ks[0].x), pair(ks[1].x)), max_pair(pair(ks[0].y), pair(ks[1].y)));
+    const int most = max((int)top2.x, (int)top2.y);
+    if (__builtin_amdgcn_ballot_w64(most - bias >= kScaleHigh) != 0 ||
+        (bias > 0 && __builtin_amdgcn_ballot_w64(most - bias >= kScaleLow) == 0)) {
+      int all = most;
+#pragma unroll
+      for (int i = 1; i < 64; i *= 2) all = max(all, __shfl_xor(all, i));
+      bias = __builtin_amdgcn_readfirstlane(max((all >> 7) - kScaleSet, 0) << 7);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) scale[r] = __builtin_amdgcn_ldexpf(a.scale_log2, (bias >> 7) - 112 - shift[r]);
+    }
+    const u16x2 off = {(unsigned short)bias, (unsigned short)bias};
+    f32x4 xs[2][NR];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f16x2 sc[KS / 2];
+#pragma unroll
+      for (int i = 0; i < KS / 2; ++i)
+        sc[i] = __builtin_bit_cast(f16x2, __builtin_elementwise_sub_sat(pair(ks[u][i]), off) << 3);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const _Float16 one = sc[s >> 1][s & 1];
+        Frag k = codes(kw[u][s], magic);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          k.w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, k.w[i]) * (f16x2){one, one});
+#pragma unroll
+        for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, qf[r][s], xs[u][r]);
+      }
+    }
+    // (after the last block, that block once more: no branch, so the registers stay in place)
+    const auto next = block_at(j + kAttnWaves < j1 ? j + kAttnWaves : j);
+    __builtin_amdgcn_sched_barrier(0);
+    load_keys(next);
 
-    const bool masked = (j + 1) * kCacheBlock > all_seen;
     Frag pf[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      float x[8];
+      float x[8], w[8];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x4 sum = {0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const f32x4 d = mfma(codes(kw[u][s]), qf[r][s], (f32x4){0, 0, 0, 0});
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sum[i] = fmaf(d[i], ks[u][i][s], sum[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[u * 4 + i] = sum[i] * scale[r];
+      for (int i = 0; i < 8; ++i) {
+        x[i] = xs[i >> 2][r][i & 3] * scale[r];
+        w[i] = __uint_as_float(vs[i >> 2][i & 3]);
       }
-      float w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = vs[i];
       if (masked) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          // what an unseen slot holds may be anything: neither its score nor its scale is used
-          const bool out = j * kCacheBlock + (i >> 2) * 16 + g * 4 + (i & 3) >= seen[r];
+          const bool out = missing || j * kCacheBlock + (i >> 2) * 16 + g * 4 + (i & 3) >= seen[r];
           x[i] = out ? -INFINITY : x[i];
           w[i] = out ? 0.0f : w[i];
         }
@@ -240,8 +290,8 @@ __global__ __launch_bounds__(kAttnThreads) void k_cache_attention(CacheAttnArgs 
       if (__builtin_amdgcn_ballot_w64(fmaxf(top, sum * kLeastScale) > kLimit) != 0) {
         float next = kNoMax;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (x[i] > -INFINITY) next = fmaxf(next, x[i] + __builtin_amdgcn_logf(fmaxf(w[i], kLeastScale)) - kSet);
+        for (int i = 0; i < 8; ++i)  // (of an unseen slot: -infinity)
+          next = fmaxf(next, x[i] + __builtin_amdgcn_logf(fmaxf(w[i], kLeastScale)) - kSet);
         next = fmaxf(next, __shfl_xor(next, 16));
         next = fmaxf(next, __shfl_xor(next, 32));
         next = fmaxf(next, m[r]);
@@ -258,10 +308,12 @@ __global__ __launch_bounds__(kAttnThreads) void k_cache_attention(CacheAttnArgs 
     }
 #pragma unroll
     for (int x = 0; x < ND; ++x) {
-      const Frag v = codes(vw[x]);
+      const Frag v = codes(vw[x >> 2][x & 3], magic);
 #pragma unroll
       for (int r = 0; r < NR; ++r) acc[r][x] = mfma(v, pf[r], acc[r][x]);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    load_values(next);
   }
 
   // join the four waves
@@ -304,9 +356,9 @@ __global__ __launch_bounds__(kAttnThreads) void k_cache_attention(CacheAttnArgs 
 #pragma unroll
         for (int w = 0; w < kAttnWaves; ++w) o[i] += lds_o[w][row16][c0 + i];
       }
-      const int t = row / a.R, hq = head * a.R + row % a.R;
+      const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
       const int64_t token = q.row + t;
-      if (rg.active == 1) {
+      if (rg.keys <= a.chunk) {  // the only chunk
         const float inv = st.y > 0.0f ? 1.0f / st.y : 0.0f;
         uint16_t* to = a.o.data + layer * a.o.layer + token * a.o.token + hq * a.o.head + c0;
 #pragma unroll
@@ -333,25 +385,26 @@ template <int D>
 __global__ __launch_bounds__(kAttnThreads) void k_cache_merge(CacheAttnArgs a) {
   constexpr int CH = D / 64;  // channels of a lane
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int heads = a.c.L * a.c.Hkv, width = 16 * a.tiles;
-  const int lh = (int)blockIdx.x % heads, rest = (int)blockIdx.x / heads;
-  const int layer = lh / a.c.Hkv, head = lh % a.c.Hkv;
+  const int width = 16 * a.tiles;
+  const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest);
+  const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
   const int b = blockIdx.y;
   const StepSeq q = step_sequence(a.c, a.s, b);
   const int row = rest * kAttnWaves + wave;
   const RowGroup rg = row_group(a, q, row / width, width);
-  if (row >= rg.rows || rg.active == 1) return;
-  const int hq = head * a.R + row % a.R;
-  const int64_t token = q.row + row / a.R;
+  if (row >= rg.rows || rg.keys <= a.chunk) return;
+  const int active = a.by_chunk.div(rg.keys + a.chunk - 1);
+  const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
+  const int64_t token = q.row + t;
   const int64_t rows = (int64_t)a.c.L * a.s.total * a.Hq;
   const int64_t at = (layer * (int64_t)a.s.total + token) * a.Hq + hq;
   float top = kNoMax;
-  for (int c = lane; c < rg.active; c += 64) top = fmaxf(top, a.stat[c * rows + at].x);
+  for (int c = lane; c < active; c += 64) top = fmaxf(top, a.stat[c * rows + at].x);
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
   float sum = 0.0f, o[CH] = {};
 #pragma unroll 4
-  for (int c = 0; c < rg.active; ++c) {
+  for (int c = 0; c < active; ++c) {
     const float2 st = a.stat[c * rows + at];
     const float f = __builtin_amdgcn_exp2f(st.x - top);
     sum += st.y * f;
@@ -370,11 +423,11 @@ __global__ __launch_bounds__(kAttnThreads) void k_cache_merge(CacheAttnArgs a) {
 
 }  // namespace
 
-CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t total,
-                     int32_t max_new, int32_t max_len) {
+CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t page_tokens, int32_t batch,
+                     int32_t total, int32_t max_new, int32_t max_len) {
   constexpr int64_t kUnit = 32 * kAttnWaves;  // tokens: a block for each wave
-  constexpr int64_t kMost = 8192;             // tokens: a wave's pages fit its lanes
   constexpr int64_t kWorkgroups = 1024;       // four for every CU
+  const int64_t kMost = std::min(64 * page_tokens, 8192);  // tokens: a chunk's pages fit a wave's lanes
   CachePlan p;
   const int64_t rows = (int64_t)(Hq / Hkv) * max_new;
   p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;

@@ -45,6 +45,21 @@ struct CacheArgs {
   int32_t L, Hkv;
 };
 
+// Division of 0 <= n < 2^31 by a d >= 1 that the host knows: a multiply and a shift (T. Granlund and P. Montgomery,
+// "Division by Invariant Integers using Multiplication", 1994), where the compiler's takes 20 instructions and
+// leaves a uniform quotient in vector registers.
+struct Divisor {
+  uint32_t d, m, l;
+  __host__ static Divisor of(int64_t d) {
+    Divisor r = {(uint32_t)d, 0, 0};
+    while (((int64_t)1 << r.l) < d) ++r.l;
+    r.m = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << r.l) - (uint64_t)d)) / (uint64_t)d + 1);
+    return r;
+  }
+  __device__ int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> l); }
+  __device__ int mod(int n, int quotient) const { return n - quotient * (int)d; }
+};
+
 // New tokens of sequence b: its rows of the step's tensors and its tokens of the cache.
 struct StepArgs {
   const int32_t* offsets;  // [batch + 1] or nullptr
@@ -53,17 +68,21 @@ struct StepArgs {
 struct StepSeq {
   int32_t row, count, len;  // first row, new tokens, tokens held (0 where the length does not count)
 };
+// An element that the whole wave reads and no kernel running beside this one writes: a scalar load.
+__device__ inline int32_t scalar_load(const int32_t* p) {
+  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
+}
 __device__ inline StepSeq step_sequence(const CacheArgs& c, const StepArgs& s, int b) {
   StepSeq q;
   q.row = b;
   q.count = 1;
   if (s.offsets != nullptr) {
-    const int32_t lo = s.offsets[b], hi = s.offsets[b + 1];
+    const int32_t lo = scalar_load(s.offsets + b), hi = scalar_load(s.offsets + b + 1);
     const bool good = lo >= 0 && hi > lo && hi <= s.total && hi - lo <= s.max_new;
     q.row = good ? lo : 0;
     q.count = good ? hi - lo : 0;
   }
-  const int32_t len = c.lens[b];
+  const int32_t len = scalar_load(c.lens + b);
   q.len = len < 0 || len > c.max_len ? 0 : len;
   return q;
 }
@@ -120,8 +139,8 @@ struct CachePlan {
   int32_t tiles, row_groups, chunk, chunks;
   size_t stat_off, o_off, total;  // workspace: (max, sum) float2 and output fp32 [D], [chunks][L * total * Hq]
 };
-CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t total,
-                     int32_t max_new, int32_t max_len);
+CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t page_tokens, int32_t batch,
+                     int32_t total, int32_t max_new, int32_t max_len);
 
 struct CacheAttnArgs {
   CacheArgs c;
@@ -130,7 +149,9 @@ struct CacheAttnArgs {
   float* lse;       // [L][Hq][total] or nullptr
   float2* stat;
   float* part;
-  int32_t Hq, R;
+  int32_t Hq;
+  Divisor R;        // query heads of a KV head
+  Divisor heads, by_Hkv, by_groups, by_chunk;  // L * Hkv, Hkv, row_groups, chunk
   float scale_log2; // softmax_scale * log2(e)
   int32_t tiles, row_groups, chunk, chunks;
 };
