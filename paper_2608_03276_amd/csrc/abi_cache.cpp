@@ -240,12 +240,12 @@ static tp_status prepare_attention(const tp_dims* dims, const tp_cache* cache, c
   a.c.max_len = (int32_t)max_len;
   a.Hq = dims->num_q_heads;
   a.R = tp::Divisor::of(dims->num_q_heads / dims->num_kv_heads);
-  const double rows = (double)dims->num_layers * dims->num_q_heads * step->total;
+  const double rows = (double)dims->num_layers * dims->num_q_heads * step->max_new * cache->batch;
   if ((double)a.R.d * step->max_new > 0x1p26 || rows > 0x1p32)
     return fail(TP_ERR_UNSUPPORTED, "step of %d tokens too long for these dims", step->total);
-  plan = tp::cache_plan(a.c.L, a.Hq, a.c.Hkv, dims->head_dim, cache->page_tokens, a.c.batch, a.s.total, a.s.max_new, a.c.max_len);
+  plan = tp::cache_plan(a.c.L, a.Hq, a.c.Hkv, dims->head_dim, a.c.batch, a.s.max_new, a.c.max_len);
   if (!fits_grid((double)dims->num_layers * dims->num_kv_heads * plan.row_groups * plan.chunks) ||
-      !fits_grid((double)dims->num_layers * dims->num_kv_heads * plan.row_groups * plan.tiles * 4.0))
+      !fits_grid((double)dims->num_layers * dims->num_kv_heads * plan.row_groups * plan.tiles * 16.0))
     return fail(TP_ERR_UNSUPPORTED, "step or sequences too long for one launch");
   a.heads = tp::Divisor::of((int64_t)dims->num_layers * dims->num_kv_heads);
   a.by_Hkv = tp::Divisor::of(dims->num_kv_heads);
@@ -255,6 +255,7 @@ static tp_status prepare_attention(const tp_dims* dims, const tp_cache* cache, c
   a.row_groups = plan.row_groups;
   a.chunk = plan.chunk;
   a.chunks = plan.chunks;
+  a.once = plan.once;
   return TP_OK;
 }
 

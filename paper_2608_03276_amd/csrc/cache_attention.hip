@@ -26,7 +26,6 @@
 namespace tp {
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -34,8 +33,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kAttnThreads = 256;
-constexpr int kAttnWaves = kAttnThreads / 64;
+constexpr int W = 4;  // waves of a workgroup
+constexpr int kAttnThreads = 64 * W, kMergeThreads = 256;
 constexpr float kNoMax = -3.402823466e38f;  // (maximum, sum) of nothing is (kNoMax, 0): joining it changes nothing
 constexpr float kLn2 = 0.6931471805599453f;
 // A row's reference is set so that its largest weight is 2^kSet, and raised when one exceeds 2^kLimit (fp16
@@ -84,6 +83,36 @@ __device__ inline Frag codes(uint32_t w, uint32_t magic) {
   return f;
 }
 
+// Reductions over the four lanes of a row (lane, lane ^ 16, ^ 32, ^ 48) and over the wave, without LDS: a swap of
+// a register with itself leaves the two sides of an exchange in its two results.
+__device__ inline u32x2 swap16(uint32_t x) { return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x, x, false, false)); }
+__device__ inline u32x2 swap32(uint32_t x) { return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(x, x, false, false)); }
+__device__ inline float row_max(float x) {
+  u32x2 s = swap16(__float_as_uint(x));
+  x = fmaxf(__uint_as_float(s.x), __uint_as_float(s.y));
+  s = swap32(__float_as_uint(x));
+  return fmaxf(__uint_as_float(s.x), __uint_as_float(s.y));
+}
+__device__ inline float row_sum(float x) {
+  u32x2 s = swap16(__float_as_uint(x));
+  x = __uint_as_float(s.x) + __uint_as_float(s.y);
+  s = swap32(__float_as_uint(x));
+  return __uint_as_float(s.x) + __uint_as_float(s.y);
+}
+__device__ inline uint32_t row_max(uint32_t x) {
+  u32x2 s = swap16(x);
+  s = swap32(max(s.x, s.y));
+  return max(s.x, s.y);
+}
+__device__ inline uint32_t wave_max(uint32_t x) {
+  // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, false));
+  return row_max(x);
+}
+
 // The keys that a group of query rows sees, and the chunks they take.
 struct RowGroup {
   int row0, rows;      // the group's first row, and the sequence's rows
@@ -99,14 +128,37 @@ __device__ inline RowGroup row_group(const CacheAttnArgs& a, const StepSeq& q, i
   return r;
 }
 
-template <int D, int NR>
-__global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k_cache_attention(CacheAttnArgs a) {
+// Place of a row's partial result: [chunks][batch][L * Hkv][R * max_new].
+__device__ inline int64_t partial_row(const CacheAttnArgs& a, int chunk, int b, int lh, int row) {
+  return (((int64_t)chunk * a.c.batch + b) * (int)a.heads.d + lh) * ((int64_t)a.R.d * a.s.max_new) + row;
+}
+
+// CH channels of a row from c0: the sum of weighted values over the sum of weights (st.y), and the log-sum-exp.
+template <int CH>
+__device__ inline void store_output(const CacheAttnArgs& a, int layer, int64_t token, int hq, int c0, const float (&o)[CH],
+                                    const float2& st) {
+  const float inv = st.y > 0.0f ? 1.0f / st.y : 0.0f;
+  uint16_t* to = a.o.data + layer * a.o.layer + token * a.o.token + hq * a.o.head + c0;
+  typedef __bf16 bf16s __attribute__((ext_vector_type(CH)));
+  bf16s v;
+#pragma unroll
+  for (int i = 0; i < CH; ++i) v[i] = (__bf16)(o[i] * inv);
+  *(bf16s*)to = v;
+  if (a.lse != nullptr && c0 == 0)
+    a.lse[((int64_t)layer * a.Hq + hq) * a.s.total + token] =
+        st.y > 0.0f ? (st.x + __builtin_amdgcn_logf(st.y)) * kLn2 : -INFINITY;
+}
+
+// NR tiles of 16 rows.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave it out).
+template <int D, int NR, bool ONCE>
+__global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache_attention(CacheAttnArgs a) {
   using B = CacheBlock<D>;
   constexpr int KS = D / 32;  // products of a score: channels in steps of 32
   constexpr int ND = D / 16;  // output tiles: channels in steps of 16
   constexpr int kStride = D + 4;
-  __shared__ float lds_o[kAttnWaves][16][kStride];
-  __shared__ float2 lds_stat[kAttnWaves][16 * NR];
+  constexpr int kPolicy = ONCE ? 2 : 0;  // nontemporal
+  __shared__ float lds_o[W][16][kStride];
+  __shared__ float2 lds_stat[W][16 * NR];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15;
@@ -114,24 +166,31 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
   const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
   const int chunk = a.by_groups.div(rest), group = a.by_groups.mod(rest, chunk);
   const int b = blockIdx.y;
-  // the chunk's pages, one a lane (a chunk has at most 64)
-  const int page0 = (chunk * a.chunk / kCacheBlock) >> a.c.page_shift;
-  int pages = page0 + lane < a.c.max_pages ? a.c.table[(int64_t)b * a.c.max_pages + page0 + lane] : -1;
+  // 64 of the chunk's pages from page0 on, one a lane
+  int page0 = (chunk * a.chunk / kCacheBlock) >> a.c.page_shift;
+  const auto load_pages = [&] {
+    return page0 + lane < a.c.max_pages ? a.c.table[(int64_t)b * a.c.max_pages + page0 + lane] : -1;
+  };
+  int pages = load_pages();
   const StepSeq q = step_sequence(a.c, a.s, b);
   const RowGroup rg = row_group(a, q, group, 16 * NR);
   if (rg.row0 >= rg.rows || (chunk > 0 && chunk * a.chunk >= rg.keys)) return;
   if (pages >= a.c.num_pages) pages = -1;
 
-  Frag qf[NR][KS];
-  int shift[NR];    // the power of two that the row was multiplied by
+  // Queries as the products' B operand: in registers, or, for several tiles, in LDS, one copy for the waves, which
+  // leaves registers for three (two tiles) or two (four) waves a SIMD.
+  constexpr bool kShared = NR > 1;
+  __shared__ u32x4 lds_q[kShared ? NR * KS * 64 : 1];
+  Frag qf[kShared ? 1 : NR][KS];
+  __shared__ int lds_shift[kShared ? 16 * NR : 1];  // the powers of two that the rows were multiplied by
+  int shift = 0;                                    // (one tile: the lane's row's)
   float scale[NR];  // softmax_scale * log2(e), less that power and the key scales'
-  int seen[NR];     // keys of the lane's row
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
+    if (kShared && r != wave) continue;  // a wave prepares one tile
     const int row = rg.row0 + r * 16 + n;
     const int t = a.R.div(row);
     const bool in = row < rg.rows;
-    seen[r] = in ? rg.before + t + 1 : 0;
     const uint16_t* p = a.q.data + layer * a.q.layer + (q.row + t) * a.q.token + (head * (int)a.R.d + a.R.mod(row, t)) * a.q.head;
     uint4 x[KS];
     uint32_t top = 0;  // the row's largest magnitude, as bf16 bits
@@ -142,20 +201,41 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
     }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    top = row_max(top);
     const int e = 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(top << 16));  // the largest comes to [2^14, 2^15)
-    shift[r] = e;
-    scale[r] = __builtin_amdgcn_ldexpf(a.scale_log2, -112 - e);
+    shift = e;
+    if (kShared && g == 0) lds_shift[r * 16 + n] = e;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const uint32_t w[4] = {x[s].x, x[s].y, x[s].z, x[s].w};
+      Frag f;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        qf[r][s].w[i] = pack_h(__builtin_amdgcn_ldexpf(__uint_as_float(w[i] << 16), e),
-                               __builtin_amdgcn_ldexpf(__uint_as_float(w[i] & 0xFFFF0000u), e));
+        f.w[i] = pack_h(__builtin_amdgcn_ldexpf(__uint_as_float(w[i] << 16), e),
+                        __builtin_amdgcn_ldexpf(__uint_as_float(w[i] & 0xFFFF0000u), e));
+      if (!kShared)
+        qf[kShared ? 0 : r][s] = f;
+      else
+        lds_q[(r * KS + s) * 64 + lane] = (u32x4){f.w[0], f.w[1], f.w[2], f.w[3]};
     }
   }
+  if (kShared) __syncthreads();
+  const auto set_scales = [&](int power) {
+#pragma unroll
+    for (int r = 0; r < NR; ++r)  // (above 0, so that an unseen token's -infinity stays one)
+      scale[r] = fmaxf(__builtin_amdgcn_ldexpf(a.scale_log2, power - (kShared ? lds_shift[r * 16 + n] : shift)), 0x1p-149f);
+  };
+  set_scales(-112);
+  const auto query = [&](int r, int s) {
+    if (!kShared) return qf[kShared ? 0 : r][s];
+    Frag f;
+    const u32x4 x = lds_q[(r * KS + s) * 64 + lane];
+    f.w[0] = x.x;
+    f.w[1] = x.y;
+    f.w[2] = x.z;
+    f.w[3] = x.w;
+    return f;
+  };
 
   uint32_t magic = 0x64006400u;
   asm("" : "+v"(magic));
@@ -191,20 +271,20 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if (KS == 4) {
-        kw[u] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_key, B::kKeys + u * 8 * D, 0);
-        ks[u] = __builtin_amdgcn_raw_buffer_load_b64(blk, at_key_scale, B::kKeyScales + u * D, 0);
+        kw[u] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_key, B::kKeys + u * 8 * D, kPolicy);
+        ks[u] = __builtin_amdgcn_raw_buffer_load_b64(blk, at_key_scale, B::kKeyScales + u * D, kPolicy);
       } else {
-        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(blk, at_key, B::kKeys + u * 8 * D, 0);
+        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(blk, at_key, B::kKeys + u * 8 * D, kPolicy);
         kw[u] = (u32x4){w.x, w.y, 0, 0};
-        ks[u] = (u32x2){__builtin_amdgcn_raw_buffer_load_b32(blk, at_key_scale, B::kKeyScales + u * D, 0), 0};
+        ks[u] = (u32x2){__builtin_amdgcn_raw_buffer_load_b32(blk, at_key_scale, B::kKeyScales + u * D, kPolicy), 0};
       }
     }
   };
   const auto load_values = [&](__amdgpu_buffer_rsrc_t blk) {
 #pragma unroll
-    for (int x = 0; x < ND / 4; ++x) vw[x] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_value, B::kValues + x * 1024, 0);
+    for (int x = 0; x < ND / 4; ++x) vw[x] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_value, B::kValues + x * 1024, kPolicy);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) vs[u] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_value_scale, B::kValueScales + u * 64, 0);
+    for (int u = 0; u < 2; ++u) vs[u] = __builtin_amdgcn_raw_buffer_load_b128(blk, at_value_scale, B::kValueScales + u * 64, kPolicy);
   };
   if (j0 < j1) {
     const auto blk = block_at(j0);
@@ -212,7 +292,7 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
     load_values(blk);
   }
   int bias = 0;  // bf16 bits taken off a key scale: it becomes an fp16 number times 2^(bias / 128 - 112)
-  for (int j = j0; j < j1; j += kAttnWaves) {
+  for (int j = j0; j < j1; j += W) {
     const bool missing = page_of(j) < 0;
     const bool masked = missing || (j + 1) * kCacheBlock > all_seen;
     if (masked) {  // scales of slots that no row sees may be anything
@@ -225,12 +305,8 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
     const int most = max((int)top2.x, (int)top2.y);
     if (__builtin_amdgcn_ballot_w64(most - bias >= kScaleHigh) != 0 ||
         (bias > 0 && __builtin_amdgcn_ballot_w64(most - bias >= kScaleLow) == 0)) {
-      int all = most;
-#pragma unroll
-      for (int i = 1; i < 64; i *= 2) all = max(all, __shfl_xor(all, i));
-      bias = __builtin_amdgcn_readfirstlane(max((all >> 7) - kScaleSet, 0) << 7);
-#pragma unroll
-      for (int r = 0; r < NR; ++r) scale[r] = __builtin_amdgcn_ldexpf(a.scale_log2, (bias >> 7) - 112 - shift[r]);
+      bias = __builtin_amdgcn_readfirstlane(max((int)(wave_max((uint32_t)most) >> 7) - kScaleSet, 0) << 7);
+      set_scales((bias >> 7) - 112);
     }
     const u16x2 off = {(unsigned short)bias, (unsigned short)bias};
     f32x4 xs[2][NR];
@@ -250,37 +326,41 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
         for (int i = 0; i < 4; ++i)
           k.w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, k.w[i]) * (f16x2){one, one});
 #pragma unroll
-        for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, qf[r][s], xs[u][r]);
+        for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, query(r, s), xs[u][r]);
       }
     }
     // (after the last block, that block once more: no branch, so the registers stay in place)
-    const auto next = block_at(j + kAttnWaves < j1 ? j + kAttnWaves : j);
+    const int jn = j + W < j1 ? j + W : j;
+    if ((jn >> a.c.page_shift) - page0 >= 64) {
+      page0 = jn >> a.c.page_shift;
+      pages = load_pages();
+      if (pages >= a.c.num_pages) pages = -1;
+    }
+    const auto next = block_at(jn);
     __builtin_amdgcn_sched_barrier(0);
     load_keys(next);
 
     Frag pf[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      float x[8], w[8];
+      float w[8], p[8], sum, top;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = xs[i >> 2][r][i & 3] * scale[r];
-        w[i] = __uint_as_float(vs[i >> 2][i & 3]);
-      }
+      for (int i = 0; i < 8; ++i) w[i] = __uint_as_float(vs[i >> 2][i & 3]);
       if (masked) {
+        const int row = rg.row0 + r * 16 + n;
+        const int seen = missing || row >= rg.rows ? 0 : rg.before + a.R.div(row) + 1;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const bool out = missing || j * kCacheBlock + (i >> 2) * 16 + g * 4 + (i & 3) >= seen[r];
-          x[i] = out ? -INFINITY : x[i];
-          w[i] = out ? 0.0f : w[i];
-        }
+        for (int i = 0; i < 8; ++i)
+          if (j * kCacheBlock + (i >> 2) * 16 + g * 4 + (i & 3) >= seen) {
+            xs[i >> 2][r][i & 3] = -INFINITY;
+            w[i] = 0.0f;  // (the slot may hold anything)
+          }
       }
-      float p[8], sum, top;
       const auto weigh = [&] {
         sum = top = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(x[i] - m[r]);
+          p[i] = __builtin_amdgcn_exp2f(fmaf(xs[i >> 2][r][i & 3], scale[r], -m[r]));
           sum += p[i];
           p[i] *= w[i];
           top = fmaxf(top, p[i]);
@@ -290,11 +370,10 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
       if (__builtin_amdgcn_ballot_w64(fmaxf(top, sum * kLeastScale) > kLimit) != 0) {
         float next = kNoMax;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)  // (of an unseen slot: -infinity)
-          next = fmaxf(next, x[i] + __builtin_amdgcn_logf(fmaxf(w[i], kLeastScale)) - kSet);
-        next = fmaxf(next, __shfl_xor(next, 16));
-        next = fmaxf(next, __shfl_xor(next, 32));
-        next = fmaxf(next, m[r]);
+        for (int i = 0; i < 8; ++i) {
+          next = fmaxf(next, fmaf(xs[i >> 2][r][i & 3], scale[r], __builtin_amdgcn_logf(fmaxf(w[i], kLeastScale)) - kSet));
+        }
+        next = fmaxf(row_max(next), m[r]);
         const float f = __builtin_amdgcn_exp2f(m[r] - next);
         m[r] = next;
         l[r] *= f;
@@ -316,11 +395,10 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
     load_values(next);
   }
 
-  // join the four waves
+  // join the waves
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    l[r] += __shfl_xor(l[r], 16);
-    l[r] += __shfl_xor(l[r], 32);
+    l[r] = row_sum(l[r]);
     if (g == 0) lds_stat[wave][r * 16 + n] = make_float2(m[r], l[r]);
   }
   __syncthreads();
@@ -328,7 +406,7 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
   for (int r = 0; r < NR; ++r) {
     float top = kNoMax;
 #pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) top = fmaxf(top, lds_stat[w][r * 16 + n].x);
+    for (int w = 0; w < W; ++w) top = fmaxf(top, lds_stat[w][r * 16 + n].x);
     const float f = __builtin_amdgcn_exp2f(m[r] - top);
     if (r > 0) __syncthreads();
 #pragma unroll
@@ -337,143 +415,160 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 2 : 1) void k
       *(f32x4*)&lds_o[wave][n][x * 16 + g * 4] = o;
     }
     __syncthreads();
-    // a row's channels by 16 threads
-    const int row16 = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * (D / 16);
+    // a row's channels by 4 W threads
+    constexpr int CH = D / (4 * W);
+    const int row16 = threadIdx.x / (4 * W), c0 = (threadIdx.x % (4 * W)) * CH;
     const int row = rg.row0 + r * 16 + row16;
     if (row < rg.rows) {
       float2 st = make_float2(kNoMax, 0.0f);
 #pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) st.x = fmaxf(st.x, lds_stat[w][r * 16 + row16].x);
+      for (int w = 0; w < W; ++w) st.x = fmaxf(st.x, lds_stat[w][r * 16 + row16].x);
 #pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float2 s = lds_stat[w][r * 16 + row16];
         st.y += s.y * __builtin_amdgcn_exp2f(s.x - st.x);
       }
-      float o[D / 16];
+      float o[CH];
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
+      for (int i = 0; i < CH; ++i) {
         o[i] = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kAttnWaves; ++w) o[i] += lds_o[w][row16][c0 + i];
+        for (int w = 0; w < W; ++w) o[i] += lds_o[w][row16][c0 + i];
       }
       const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
       const int64_t token = q.row + t;
       if (rg.keys <= a.chunk) {  // the only chunk
-        const float inv = st.y > 0.0f ? 1.0f / st.y : 0.0f;
-        uint16_t* to = a.o.data + layer * a.o.layer + token * a.o.token + hq * a.o.head + c0;
-#pragma unroll
-        for (int i = 0; i < D / 16; i += 2) {
-          const bf16x2 two = {(__bf16)(o[i] * inv), (__bf16)(o[i + 1] * inv)};
-          *(bf16x2*)(to + i) = two;
-        }
-        if (a.lse != nullptr && (threadIdx.x & 15) == 0)
-          a.lse[((int64_t)layer * a.Hq + hq) * a.s.total + token] =
-              st.y > 0.0f ? (st.x + __builtin_amdgcn_logf(st.y)) * kLn2 : -INFINITY;
+        store_output<CH>(a, layer, token, hq, c0, o, st);
       } else {
-        const int64_t rows = (int64_t)a.c.L * a.s.total * a.Hq;
-        const int64_t at = chunk * rows + (layer * (int64_t)a.s.total + token) * a.Hq + hq;
-        if ((threadIdx.x & 15) == 0) a.stat[at] = st;
+        const int64_t at = partial_row(a, chunk, b, lh, row);
+        if (c0 == 0) a.stat[at] = st;
 #pragma unroll
-        for (int i = 0; i < D / 16; i += 4) *(f32x4*)(a.part + at * D + c0 + i) = (f32x4){o[i], o[i + 1], o[i + 2], o[i + 3]};
+        for (int i = 0; i < CH; ++i) a.part[at * D + c0 + i] = o[i];
       }
     }
   }
 }
 
-// Joins the chunks of a row: one wave each.
-template <int D>
-__global__ __launch_bounds__(kAttnThreads) void k_cache_merge(CacheAttnArgs a) {
-  constexpr int CH = D / 64;  // channels of a lane
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Joins the chunks of a row: by WPR waves, whose groups of D / 4 lanes take every kGroups-th chunk, four channels a
+// lane, each with a reference of its own.
+template <int D, int WPR>
+__global__ __launch_bounds__(kMergeThreads) void k_cache_merge(CacheAttnArgs a) {
+  constexpr int kLanes = D / 4;
+  constexpr int kGroups = WPR * 64 / kLanes;
+  constexpr int kRows = kMergeThreads / 64 / WPR;
+  __shared__ f32x4 lds_o[kRows][kGroups][kLanes];
+  __shared__ float2 lds_stat[kRows][kGroups];
   const int width = 16 * a.tiles;
   const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest);
   const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
   const int b = blockIdx.y;
+  const int mine = threadIdx.x / (WPR * 64);                      // row of the workgroup
+  const int part = threadIdx.x % (WPR * 64) / kLanes, lane = threadIdx.x % kLanes;
   const StepSeq q = step_sequence(a.c, a.s, b);
-  const int row = rest * kAttnWaves + wave;
+  const int row = rest * kRows + mine;
   const RowGroup rg = row_group(a, q, row / width, width);
-  if (row >= rg.rows || rg.keys <= a.chunk) return;
-  const int active = a.by_chunk.div(rg.keys + a.chunk - 1);
+  const bool in = row < rg.rows && rg.keys > a.chunk;
   const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
   const int64_t token = q.row + t;
-  const int64_t rows = (int64_t)a.c.L * a.s.total * a.Hq;
-  const int64_t at = (layer * (int64_t)a.s.total + token) * a.Hq + hq;
-  float top = kNoMax;
-  for (int c = lane; c < active; c += 64) top = fmaxf(top, a.stat[c * rows + at].x);
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
-  float sum = 0.0f, o[CH] = {};
+  const int64_t at = partial_row(a, 0, b, lh, row), rows = partial_row(a, 1, 0, 0, 0);
+  float2 st = make_float2(kNoMax, 0.0f);
+  f32x4 o = {0, 0, 0, 0};
+  if (in) {
+    const int active = a.by_chunk.div(rg.keys + a.chunk - 1);
 #pragma unroll 4
-  for (int c = 0; c < active; ++c) {
-    const float2 st = a.stat[c * rows + at];
-    const float f = __builtin_amdgcn_exp2f(st.x - top);
-    sum += st.y * f;
-    const float* p = a.part + (c * rows + at) * D + lane * CH;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) o[i] = fmaf(p[i], f, o[i]);
+    for (int c = part; c < active; c += kGroups) {
+      const float2 s = a.stat[c * rows + at];
+      const f32x4 p = *(const f32x4*)(a.part + (c * rows + at) * D + lane * 4);
+      const float top = fmaxf(st.x, s.x);
+      const float f = __builtin_amdgcn_exp2f(st.x - top), fs = __builtin_amdgcn_exp2f(s.x - top);
+      st = make_float2(top, st.y * f + s.y * fs);
+      o = o * f + p * fs;
+    }
+    lds_o[mine][part][lane] = o;
+    if (lane == 0) lds_stat[mine][part] = st;
   }
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  uint16_t* to = a.o.data + layer * a.o.layer + token * a.o.token + hq * a.o.head + lane * CH;
+  __syncthreads();
+  if (!in || part != 0) return;
+  float top = kNoMax;
 #pragma unroll
-  for (int i = 0; i < CH; ++i) to[i] = __builtin_bit_cast(uint16_t, (__bf16)(o[i] * inv));
-  if (a.lse != nullptr && lane == 0)
-    a.lse[((int64_t)layer * a.Hq + hq) * a.s.total + token] =
-        sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  for (int i = 0; i < kGroups; ++i) top = fmaxf(top, lds_stat[mine][i].x);
+  st = make_float2(top, 0.0f);
+  o = (f32x4){0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    const float2 s = lds_stat[mine][i];
+    const float f = __builtin_amdgcn_exp2f(s.x - top);
+    st.y += s.y * f;
+    o += lds_o[mine][i][lane] * f;
+  }
+  const float x[4] = {o.x, o.y, o.z, o.w};
+  store_output<4>(a, layer, token, hq, lane * 4, x, st);
 }
 
 }  // namespace
 
-CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t page_tokens, int32_t batch,
-                     int32_t total, int32_t max_new, int32_t max_len) {
-  constexpr int64_t kUnit = 32 * kAttnWaves;  // tokens: a block for each wave
-  constexpr int64_t kWorkgroups = 1024;       // four for every CU
-  const int64_t kMost = std::min(64 * page_tokens, 8192);  // tokens: a chunk's pages fit a wave's lanes
+// Chunks: merging costs a launch (4 us) and, for each row and chunk, 4 d + 8 bytes written and read.
+//  - Rows of one or two tiles (decoding, drafts): chunks of 4096 tokens where the (sequence, head) pairs alone
+//    occupy every CU (32 sequences of 8 heads and 2049 to 2548 tokens: 27.2 us whole, 29.9 in chunks of 640);
+//    otherwise about 1024 workgroups, in chunks of 512 at least (one sequence of 13215, 8 heads: 11.1 us at 512, 13.5
+//    at 1024, 25.9 at 4096; two of 262144 and 131073: 78.0 us at 4096, 92.1 at 1024, 94.1 at 8192).
+//  - Four tiles (prompts): whole sequences from 1024 workgroups on, fewer are brought to that number.
+CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
+                     int32_t max_len) {
+  constexpr int64_t kUnit = 32 * W;  // tokens: a block for each wave
+  constexpr int64_t kLeast = 512, kWhole = 4096, kWorkgroups = 1024, kCus = 256;
   CachePlan p;
   const int64_t rows = (int64_t)(Hq / Hkv) * max_new;
   p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   p.row_groups = (int32_t)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
-  const int64_t units = (int64_t)L * Hkv * batch * p.row_groups;
-  const int64_t all_rows = (int64_t)L * Hq * total;
-  // The workspace holds a partial result of every row for each chunk of the longest allowed length, or as
-  // many as the chunks of kWorkgroups workgroups of 64 rows give: a bound that grows with every argument.
-  // The chunks stay within it.
-  const int64_t least = (max_len + kMost - 1) / kMost;
-  const int64_t finest = (max_len + kUnit - 1) / kUnit;
-  int64_t partials = std::max(all_rows * least, std::min(all_rows * finest, all_rows + 64 * kWorkgroups));
-  int64_t chunks = std::max(least, std::min(finest, (kWorkgroups + units - 1) / units));
-  chunks = std::max<int64_t>(least, std::min(chunks, partials / all_rows));
+  const int64_t heads = (int64_t)L * Hkv * batch, units = heads * p.row_groups;
+  const int64_t finest = (max_len + kLeast - 1) / kLeast, whole = (max_len + kWhole - 1) / kWhole;
+  const int64_t fill = std::min(finest, (kWorkgroups + units - 1) / units);
+  int64_t chunks = p.tiles == 4 ? fill : units >= kCus ? whole : std::max(whole, fill);
   p.chunk = (int32_t)(((max_len + chunks - 1) / chunks + kUnit - 1) / kUnit * kUnit);
   p.chunks = (int32_t)((max_len + p.chunk - 1) / p.chunk);
-  if (finest == 1) partials = 0;  // one chunk whatever the plan
+  // Partial rows: up to 32 a pair in chunks of kWhole, up to 64 (kWorkgroups + units) in the fill.  The bound
+  // grows with every argument, so a buffer for the longest call serves the others.
+  const int64_t partials = finest == 1 ? 0 : std::min(heads * rows * finest, 128 * kWorkgroups + 32 * heads * whole);
+  p.once = p.row_groups == 1 &&
+           (double)heads * max_len * (double)(cache_block_bytes(head_dim) / kCacheBlock) > (double)(256 << 20);
   p.stat_off = 0;
   p.o_off = ((size_t)partials * sizeof(float2) + 255) / 256 * 256;
   p.total = p.o_off + (size_t)partials * head_dim * sizeof(float);
   return p;
 }
 
-hipError_t launch_cache_attention(const CacheAttnArgs& a, int head_dim, hipStream_t stream) {
-  const int heads = a.c.L * a.c.Hkv;
-  const dim3 grid((unsigned)(heads * a.row_groups * a.chunks), (unsigned)a.c.batch);
-#define TP_CACHE_ATTENTION(D_, NR_) \
-  hipLaunchKernelGGL((k_cache_attention<D_, NR_>), grid, dim3(kAttnThreads), 0, stream, a)
-  if (head_dim == 128) {
-    if (a.tiles == 1) TP_CACHE_ATTENTION(128, 1);
-    else if (a.tiles == 2) TP_CACHE_ATTENTION(128, 2);
-    else TP_CACHE_ATTENTION(128, 4);
-  } else {
-    if (a.tiles == 1) TP_CACHE_ATTENTION(64, 1);
-    else if (a.tiles == 2) TP_CACHE_ATTENTION(64, 2);
-    else TP_CACHE_ATTENTION(64, 4);
-  }
-#undef TP_CACHE_ATTENTION
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.chunks == 1) return e;
-  const dim3 merge((unsigned)(heads * a.row_groups * a.tiles * 16 / kAttnWaves), (unsigned)a.c.batch);
-  if (head_dim == 128)
-    hipLaunchKernelGGL(k_cache_merge<128>, merge, dim3(kAttnThreads), 0, stream, a);
+namespace {
+
+template <int D, int NR>
+void launch_part(const CacheAttnArgs& a, dim3 grid, hipStream_t stream) {
+  if (a.once)
+    hipLaunchKernelGGL((k_cache_attention<D, NR, true>), grid, dim3(kAttnThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL(k_cache_merge<64>, merge, dim3(kAttnThreads), 0, stream, a);
+    hipLaunchKernelGGL((k_cache_attention<D, NR, false>), grid, dim3(kAttnThreads), 0, stream, a);
+}
+
+template <int D>
+hipError_t launch_attention(const CacheAttnArgs& a, hipStream_t stream) {
+  const unsigned heads = (unsigned)(a.c.L * a.c.Hkv), batch = (unsigned)a.c.batch;
+  const dim3 grid(heads * a.row_groups * a.chunks, batch);
+  if (a.tiles == 1) launch_part<D, 1>(a, grid, stream);
+  else if (a.tiles == 2) launch_part<D, 2>(a, grid, stream);
+  else launch_part<D, 4>(a, grid, stream);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.chunks == 1) return e;
+  const unsigned rows = heads * a.row_groups * a.tiles * 16;  // 16 a tile
+  if (a.chunks >= 8)
+    hipLaunchKernelGGL((k_cache_merge<D, 4>), dim3(rows, batch), dim3(kMergeThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_cache_merge<D, 1>), dim3(rows / 4, batch), dim3(kMergeThreads), 0, stream, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache_attention(const CacheAttnArgs& a, int head_dim, hipStream_t stream) {
+  return head_dim == 128 ? launch_attention<128>(a, stream) : launch_attention<64>(a, stream);
 }
 
 }  // namespace tp

@@ -132,15 +132,16 @@ struct CacheReadArgs {
 };
 hipError_t launch_cache_read(const CacheReadArgs& a, int head_dim, hipStream_t stream);
 
-// The attention's plan: `tiles` tiles of 16 query rows a workgroup (rows of a KV head: new token, then
-// query head of its group), `row_groups` of them for max_new tokens; context in `chunks` chunks of `chunk`
-// tokens (a multiple of 128), whose partial results are merged when there are several.
+// The attention's plan: `tiles` tiles of 16 query rows a workgroup (rows of a KV head: new token, then query head of
+// its group), `row_groups` of them for max_new tokens; context in `chunks` chunks of `chunk` tokens (a multiple of
+// 128), whose partial results are merged when there are several.
 struct CachePlan {
   int32_t tiles, row_groups, chunk, chunks;
-  size_t stat_off, o_off, total;  // workspace: (max, sum) float2 and output fp32 [D], [chunks][L * total * Hq]
+  int32_t once;  // whether the loads leave the caches alone: the cache is read once a call, and no call finds it there
+  size_t stat_off, o_off, total;  // workspace: (max, sum) float2 and output fp32 [D] of each row and chunk
 };
-CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t page_tokens, int32_t batch,
-                     int32_t total, int32_t max_new, int32_t max_len);
+CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
+                     int32_t max_len);
 
 struct CacheAttnArgs {
   CacheArgs c;
@@ -153,7 +154,7 @@ struct CacheAttnArgs {
   Divisor R;        // query heads of a KV head
   Divisor heads, by_Hkv, by_groups, by_chunk;  // L * Hkv, Hkv, row_groups, chunk
   float scale_log2; // softmax_scale * log2(e)
-  int32_t tiles, row_groups, chunk, chunks;
+  int32_t tiles, row_groups, chunk, chunks, once;
 };
 hipError_t launch_cache_attention(const CacheAttnArgs& a, int head_dim, hipStream_t stream);
 

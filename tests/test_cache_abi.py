@@ -145,10 +145,11 @@ def test_attention_refusals():
         assert _attend(scale=scale) == B.TP_ERR_PARAM
     assert _attend(most=0) == _attend(most=321) == B.TP_ERR_SHAPE
     assert _attend(lse=FAKE + 2) == B.TP_ERR_PARAM
-    assert _attend(ws=None) == _attend(wsb=0) == _attend(ws=FAKE + 16) == B.TP_ERR_WORKSPACE
+    wide = cache(cols=64)  # 4096 tokens: partial results of several chunks
     n = ctypes.c_size_t(0)
-    assert lib.tp_cache_workspace_size(ref(D), ref(cache()), ref(step()), 320, ctypes.byref(n)) == B.TP_OK
-    assert _attend(wsb=n.value - 1) == B.TP_ERR_WORKSPACE
+    assert lib.tp_cache_workspace_size(ref(D), ref(wide), ref(step()), 4096, ctypes.byref(n)) == B.TP_OK and n.value > 0
+    for kw in (dict(ws=None), dict(wsb=0), dict(ws=FAKE + 16), dict(wsb=n.value - 1)):
+        assert _attend(c=wide, most=4096, **kw) == B.TP_ERR_WORKSPACE, kw
     assert lib.tp_cache_workspace_size(ref(D), ref(cache()), ref(step()), 320, None) == B.TP_ERR_NULL
     assert lib.tp_cache_workspace_size(ref(D), ref(cache()), ref(step()), 321, ctypes.byref(n)) == B.TP_ERR_SHAPE
     big = step(total=2 ** 31 - 1, most=2 ** 31 - 1)
