@@ -98,8 +98,8 @@ tp_status check_rows(const tp_dims* d, int32_t heads, int32_t total, const tp_ro
   return TP_OK;
 }
 
-// A launch's x dimension holds fewer than 2^32 work-items, in workgroups of 256.
-bool fits_grid(double workgroups) { return workgroups < 16777216.0; }
+// A launch's x dimension holds fewer than 2^32 work-items.
+bool fits_grid(double workgroups, double threads = 256.0) { return workgroups * threads < 0x1p32; }
 
 // Makes the stream's device current for the launch, and the caller's again afterwards.
 class OnDevice {
@@ -213,11 +213,10 @@ tp_status tp_cache_append(const tp_dims* dims, const tp_cache* cache, const tp_s
       return fail(TP_ERR_SHAPE, "q_out on q's memory must have q's strides");
   }
   a.Hq = dims->num_q_heads;
-  a.ro = tp::recip_offsets_for(7.0f);
   // n consecutive tokens lie in at most (n + 30) / 32 + 1 blocks
   a.blocks = (int32_t)(((int64_t)step->max_new + tp::kCacheBlock - 2) / tp::kCacheBlock + 1);
   const double heads = (double)dims->num_layers * dims->num_kv_heads;
-  if (!fits_grid(heads * a.blocks * cache->batch + (double)dims->num_layers * step->total))
+  if (!fits_grid(heads * a.blocks * cache->batch + (q ? (double)dims->num_layers * step->total : 0.0), 512.0))
     return fail(TP_ERR_UNSUPPORTED, "step too long for one launch");
   OnDevice on((hipStream_t)stream);
   const hipError_t e = tp::launch_cache_append(a, dims->head_dim, (hipStream_t)stream);

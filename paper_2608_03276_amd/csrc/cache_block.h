@@ -113,24 +113,25 @@ struct CacheWriteArgs {
   int32_t rotary_dim, pairs;
   int32_t Hq;
   int32_t blocks;            // blocks that a sequence's new tokens may lie in
-  RecipOffsets ro;           // of qmax 7
+  Divisor heads, by_Hkv, by_blocks, by_total;  // set by the launch
   // tp_cache_load: sequence b's tokens are rows [kept_off[b], kept_off[b + 1]) of contiguous head-major tensors
   const uint8_t* v_q;        // [L][Hkv][K_tot][D / 2]
   const float* v_scales;     // [L][Hkv][K_tot]
   int64_t kept_off[TP_MAX_BATCH + 1];
 };
-hipError_t launch_cache_append(const CacheWriteArgs& a, int head_dim, hipStream_t stream);
-hipError_t launch_cache_load(const CacheWriteArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_cache_append(CacheWriteArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_cache_load(CacheWriteArgs& a, int head_dim, hipStream_t stream);
 
 struct CacheReadArgs {
   CacheArgs c;
   uint16_t* k;  // bf16 [L][Hkv][N_tot][D]
   uint16_t* v;
   int32_t blocks;
+  Divisor heads, by_Hkv;  // set by the launch
   int64_t off[TP_MAX_BATCH + 1];
   int64_t first[TP_MAX_BATCH];
 };
-hipError_t launch_cache_read(const CacheReadArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_cache_read(CacheReadArgs& a, int head_dim, hipStream_t stream);
 
 // The attention's plan: `tiles` tiles of 16 query rows a workgroup (rows of a KV head: new token, then query head of
 // its group), `row_groups` of them for max_new tokens; context in `chunks` chunks of `chunk` tokens (a multiple of

@@ -1,9 +1,11 @@
 // Rows into and out of the paged 4-bit cache: tp_cache_append, tp_cache_load, tp_cache_read.
 //
 // One workgroup handles one block (32 tokens of one head): d/8 lanes hold a row, 16 bytes each.  The
-// value codes of a block are transposed in LDS, since a word holds one channel of eight tokens; words
-// of which only some tokens are written are read, merged and written back.  A block belongs to one
-// workgroup of the launch, so nothing races.
+// value codes of a block are transposed, since a word holds one channel of eight tokens: eight words of
+// eight channels become eight words of eight tokens in registers (32 operations), and go out by way of LDS, 16
+// bytes a lane.  A block of which only some tokens are written is read before and merged.  A block belongs to
+// one workgroup of the launch, so nothing races.  Everything that a workgroup loads hangs on the sequence's
+// offsets and length alone, but for the angles (on the positions) and the old values (on the page).
 #include "cache_block.h"
 #include "quant_row.h"
 
@@ -11,6 +13,10 @@ namespace tp {
 namespace {
 
 constexpr int kRowsThreads = 256;
+// Threads of a step's append, and where it is of more than one block a sequence: with one token the time is the chain
+// of loads and the instructions fetched, so a block is one pass of 512 threads at d = 128 (64 sequences: 6.6 us; 256
+// threads in two passes 7.2); long steps want loads in flight (12290 tokens of 64 heads: 222 us; 110).
+constexpr int kFewThreads = 512, kFewTokens = 32;
 constexpr float kMaxBf16 = 3.3895313892515355e38f;
 
 // The nibble of element e (0..7) of a word.
@@ -34,47 +40,94 @@ __device__ inline float for_bf16(float f, float rest) {
   return __uint_as_float((rest > 0.0f) == ((int32_t)b >= 0) ? b + 1 : b - 1);
 }
 
-// For rounding to bf16 once; within its range, so that no rotation of finite rows gives an infinity.
-__device__ inline float rounded(double r) {
+// Angles of 8 channels (of 4 pairs): cosines, and sines with the sign of the partner's term.
+struct Angles {
+  float c[8], s[8];
+};
+
+// The lane's part of a rotation: no angles where the piece is not rotated.
+__device__ inline bool rotates(const CacheWriteArgs& a, int piece) { return piece * 8 < a.rotary_dim; }
+// The piece whose channels are the partners' (half-split pairs).
+__device__ inline int partner(const CacheWriteArgs& a, int piece) {
+  const int half = a.rotary_dim / 16;
+  return piece < half ? piece + half : piece - half;
+}
+__device__ inline Angles load_angles(const CacheWriteArgs& a, const float* cs, int piece) {
+  const int half = a.rotary_dim / 2;
+  Angles g;
+  if (a.pairs) {
+    const float4 c = *(const float4*)(cs + piece * 4), s = *(const float4*)(cs + half + piece * 4);
+    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      g.c[i] = cc[i / 2];
+      g.s[i] = (i & 1) ? ss[i / 2] : -ss[i / 2];
+    }
+  } else {
+    const bool first = piece * 8 < half;
+    const int at = first ? piece * 8 : piece * 8 - half;
+    const float4 c0 = *(const float4*)(cs + at), c1 = *(const float4*)(cs + at + 4);
+    const float4 s0 = *(const float4*)(cs + half + at), s1 = *(const float4*)(cs + half + at + 4);
+    const float cc[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+    const float ss[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      g.c[i] = cc[i];
+      g.s[i] = first ? -ss[i] : ss[i];
+    }
+  }
+  return g;
+}
+
+// x c + y s in 64 bits (a product of a bf16 and an fp32 number is exact there), for rounding to bf16 once;
+// within its range, so that no rotation of finite rows gives an infinity.
+__device__ inline float rotated64(float x, float y, float c, float s) {
+  double r = (double)x * (double)c + (double)y * (double)s;
   r = __builtin_fmax(__builtin_fmin(r, (double)kMaxBf16), -(double)kMaxBf16);
   const float f = (float)r;
   const double rest = r - (double)f;
   return for_bf16(f, rest > 0.0 ? 1.0f : rest < 0.0 ? -1.0f : 0.0f);
 }
 
-// Piece `piece` (8 channels) of a row, rotated by the angles of the row cs of the table.  In 64 bits
-// (a product of a bf16 and an fp32 number is exact there): the codes behind it are those of the exact
-// rotation, and the kernels are bound by memory all the same.
-__device__ inline uint4 rotated_piece(const CacheWriteArgs& a, const uint16_t* row, int piece, const float* cs) {
-  const uint4 x = *((const uint4*)row + piece);
-  if (piece * 8 >= a.rotary_dim) return x;
-  const int half = a.rotary_dim / 2;
-  const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-  uint32_t out[4];
-  if (a.pairs) {
-    const float4 c = *(const float4*)(cs + piece * 4), s = *(const float4*)(cs + half + piece * 4);
-    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+// Eight channels x, rotated with their partners' y (for pairs of neighbours, y = x).  The fp32 result r is off by
+// at most 2^-24 (|x c| + 2 |y s|), r - delta and r + delta by 2^-24 (|x c| + |y s|) more; delta is 3.1 * 2^-24
+// (|x c| + |y s|), and 2^-147 for subnormal numbers.  Where r - delta and r + delta round to the same bf16 number, so does the exact value.  A wave with a
+// channel where they do not (1 in 10, of 512 channels each) forms its channels in 64 bits, at six times the
+// instructions.
+__device__ inline uint4 rotated(bool pairs, const uint4& x4, const uint4& y4, const Angles& g) {
+  const uint32_t xw[4] = {x4.x, x4.y, x4.z, x4.w}, yw[4] = {y4.x, y4.y, y4.z, y4.w};
+  float x[8], y[8];
+  uint32_t out[4], unsure = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const double p = bf16_lo(xw[i]), q = bf16_hi(xw[i]), ci = cc[i], si = ss[i];
-      out[i] = pack_bf16(rounded(p * ci - q * si), rounded(q * ci + p * si));
-    }
-  } else {
-    const bool first = piece * 8 < half;
-    const int at = first ? piece * 8 : piece * 8 - half;
-    const uint4 y = *((const uint4*)row + (first ? piece + half / 8 : piece - half / 8));
-    const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
-    const float4 c0 = *(const float4*)(cs + at), c1 = *(const float4*)(cs + at + 4);
-    const float4 s0 = *(const float4*)(cs + half + at), s1 = *(const float4*)(cs + half + at + 4);
-    const float cc[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-    const float ss[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = bf16_lo(xw[i]);
+    x[2 * i + 1] = bf16_hi(xw[i]);
+    y[2 * i] = pairs ? x[2 * i + 1] : bf16_lo(yw[i]);
+    y[2 * i + 1] = pairs ? x[2 * i] : bf16_hi(yw[i]);
+  }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const double p0 = bf16_lo(xw[i]), p1 = bf16_hi(xw[i]), q0 = bf16_lo(yw[i]), q1 = bf16_hi(yw[i]);
-      const double g0 = first ? -(double)ss[2 * i] : (double)ss[2 * i];
-      const double g1 = first ? -(double)ss[2 * i + 1] : (double)ss[2 * i + 1];
-      out[i] = pack_bf16(rounded(p0 * (double)cc[2 * i] + q0 * g0), rounded(p1 * (double)cc[2 * i + 1] + q1 * g1));
+  for (int i = 0; i < 4; ++i) {
+    float lo[2], hi[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int k = 2 * i + e;
+      const float p = y[k] * g.s[k], r = fmaf(x[k], g.c[k], p);
+      const float sum = fmaf(fabsf(x[k]), fabsf(g.c[k]), fabsf(p));
+      const float delta = fmaf(sum, 0x1.9p-23f, fminf(sum, 0x1p-147f));  // (0 of zeros)
+      lo[e] = r - delta;
+      hi[e] = r + delta;
     }
+    out[i] = pack_bf16(lo[0], lo[1]);
+    unsure |= out[i] ^ pack_bf16(hi[0], hi[1]);
+  }
+  // (an infinity or NaN of the bounds shows as a magnitude from 0x7F80 on)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unsure |= (out[i] & 0x7F80u) == 0x7F80u || (out[i] & 0x7F800000u) == 0x7F800000u;
+  if (__builtin_amdgcn_ballot_w64(unsure != 0) != 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      out[i] = pack_bf16(rotated64(x[2 * i], y[2 * i], g.c[2 * i], g.s[2 * i]),
+                         rotated64(x[2 * i + 1], y[2 * i + 1], g.c[2 * i + 1], g.s[2 * i + 1]));
   }
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
@@ -83,7 +136,8 @@ __device__ inline uint4 rotated_piece(const CacheWriteArgs& a, const uint16_t* r
 // group and call together.  The quotient v / g of bf16 numbers lies 2^-9 or more from a half unless it
 // is one (2 v - c g, c odd, is a multiple of the smaller of their units in the last place), so a product
 // with the reciprocal, off by at most 2^-20, rounds right once it is put on the grid of 2^-11, where
-// every half lies.
+// every half lies: the first addition does that, the second rounds to an integer, whose low bits are
+// the code.
 __device__ inline uint32_t key_codes(const uint4& x, uint32_t& scale_bits) {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -96,19 +150,79 @@ __device__ inline uint32_t key_codes(const uint4& x, uint32_t& scale_bits) {
   mx = max(mx, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mx, 0x4E, 0xF, 0xF, false));
   scale_bits = pack_bf16(__uint_as_float(mx << 16) / 7.0f, 0.0f);
   const float g = __uint_as_float(scale_bits << 16);
-  if (g == 0.0f) return 0x88888888u;
-  // both brought near 1 by a power of two (exact), so that no reciprocal overflows
-  const int e = -__builtin_amdgcn_frexp_expf(g);
-  const float y = 1.0f / __builtin_amdgcn_ldexpf(g, e);
   uint32_t word = 0;
+  if (__builtin_amdgcn_ballot_w64(g != 0.0f && (g < 0x1p-100f || g > 0x1p100f)) == 0) {
+    const float y = g == 0.0f ? 0.0f : 1.0f / g;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float v = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
-    const float t = (__builtin_amdgcn_ldexpf(v, e) * y + 6144.0f) - 6144.0f;  // the grid of 2^-11: 1.5 * 2^12
-    const int c = (int)__builtin_amdgcn_fmed3f(__builtin_rintf(t), -7.0f, 7.0f);
-    word |= (uint32_t)(c + 8) << (4 * nibble_of(i));
+    for (int i = 0; i < 8; ++i) {
+      const float v = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+      // 1.5 * 2^12, then up to 1.5 * 2^23 + 8
+      const uint32_t c = __float_as_uint((v * y + 6144.0f) + (12582912.0f - 6144.0f + 8.0f));
+      word |= (c & 0xFu) << (4 * nibble_of(i));
+    }
+  } else if (g == 0.0f) {
+    word = 0x88888888u;
+  } else {
+    // both brought near 1 by a power of two (exact), so that no reciprocal overflows; a subnormal scale may be
+    // rounded down so far that codes have to be clamped
+    const int e = -__builtin_amdgcn_frexp_expf(g);
+    const float y = 1.0f / __builtin_amdgcn_ldexpf(g, e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+      const float t = (__builtin_amdgcn_ldexpf(v, e) * y + 6144.0f) - 6144.0f;
+      const int c = (int)__builtin_amdgcn_fmed3f(__builtin_rintf(t), -7.0f, 7.0f);
+      word |= (uint32_t)(c + 8) << (4 * nibble_of(i));
+    }
   }
   return word;
+}
+
+// Codes (one word, element i in nibble i, two's complement) and scale of 8 channels of a value, as
+// quant_piece's for rows outside its common path: no tables to build for a few tokens.
+template <int LPT>
+__device__ inline uint32_t value_codes(const uint4& x, float& gamma) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  const QuantFmt f{true, true, 7.0f};
+  const uint32_t mx = row_absmax_bits<LPT>(w);
+  const int ef = (int)(mx >> 7);
+  gamma = __uint_as_float(mx << 16) / 7.0f;
+  uint32_t code[8], word = 0;
+  if (__builtin_amdgcn_ballot_w64(ef <= 27) != 0 && ef <= 27) {
+    codes_divided(w, gamma, f, code);
+  } else {
+    const float sc = __builtin_amdgcn_ldexpf(1.0f, 127 - ef);
+    const float gs = gamma * sc;
+    codes_scaled(w, sc, gs, 1.0f / gs, f, code);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) word |= (code[i] & 0xFu) << (4 * i);
+  return word;
+}
+
+// Words of 8 tokens' channels (element t of the tokens in nibble nibble_of(t)) from 8 tokens' words of 8
+// channels (channel i in nibble i): an 8 x 8 transpose of nibbles, halves, then bytes, then nibbles.
+__device__ inline void transpose(const uint32_t (&in)[8], uint32_t (&out)[8]) {
+  uint32_t a[8], b[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) a[nibble_of(t)] = in[t];  // row n becomes nibble n
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    b[n] = __builtin_amdgcn_perm(a[n + 4], a[n], 0x05040100u);
+    b[n + 4] = __builtin_amdgcn_perm(a[n + 4], a[n], 0x07060302u);
+  }
+#pragma unroll
+  for (int n = 0; n < 8; n += 4)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      a[n + k] = __builtin_amdgcn_perm(b[n + k + 2], b[n + k], 0x06020400u);
+      a[n + k + 2] = __builtin_amdgcn_perm(b[n + k + 2], b[n + k], 0x07030501u);
+    }
+#pragma unroll
+  for (int n = 0; n < 8; n += 2) {
+    out[n] = (a[n] & 0x0F0F0F0Fu) | ((a[n + 1] & 0x0F0F0F0Fu) << 4);
+    out[n + 1] = ((a[n] >> 4) & 0x0F0F0F0Fu) | (a[n + 1] & 0xF0F0F0F0u);
+  }
 }
 
 // Largest b with offsets[b] <= row, over batch + 1 nondecreasing entries; -1 if there is none.  The wave
@@ -127,41 +241,54 @@ __device__ inline int sequence_of(const int32_t* offsets, int batch, int32_t row
   }
 }
 
-// One token's query rows.
-template <int D>
+// One token's query rows.  The loads come first, then what decides whether they count.
+template <int D, int T>
 __device__ inline void rotate_queries(const CacheWriteArgs& a, int unit) {
-  constexpr int LPT = D / 8;
-  const int layer = unit / a.s.total, row = unit % a.s.total;
+  constexpr int LPT = D / 8, kHeads = T / LPT;
+  const int layer = a.by_total.div(unit), row = a.by_total.mod(unit, layer);
+  const int piece = threadIdx.x % LPT;
+  const bool turn = rotates(a, piece);
+  const int other = turn && !a.pairs ? partner(a, piece) : piece;
+  const uint16_t* from = a.q.data + layer * a.q.layer + row * a.q.token;
+  uint16_t* to = a.q_out.data + layer * a.q_out.layer + row * a.q_out.token;
+  int h = (int)threadIdx.x / LPT;
+  uint4 x = make_uint4(0, 0, 0, 0), y = x;
+  if (h < a.Hq) {
+    x = *((const uint4*)(from + h * a.q.head) + piece);
+    y = *((const uint4*)(from + h * a.q.head) + other);
+  }
+  const int64_t pos = scalar_load(a.positions + row);
+  if (pos < 0 || pos >= a.num_positions) return;
+  Angles g = {};
+  if (turn) g = load_angles(a, a.cos_sin + pos * a.rotary_dim, piece);
   const int b = a.s.offsets == nullptr ? row : sequence_of(a.s.offsets, a.c.batch, row);
   if (b < 0 || b >= a.c.batch) return;
   const StepSeq q = step_sequence(a.c, a.s, b);
   if (row < q.row || row - q.row >= q.count) return;
-  const int64_t pos = a.positions[row];
-  if (pos < 0 || pos >= a.num_positions) return;
-  const float* cs = a.cos_sin + pos * a.rotary_dim;
-  const int piece = threadIdx.x % LPT;
-  for (int h = threadIdx.x / LPT; h < a.Hq; h += kRowsThreads / LPT) {
-    const uint16_t* from = a.q.data + layer * a.q.layer + row * a.q.token + h * a.q.head;
-    const uint4 x = rotated_piece(a, from, piece, cs);
-    *((uint4*)(a.q_out.data + layer * a.q_out.layer + row * a.q_out.token + h * a.q_out.head) + piece) = x;
+  while (h < a.Hq) {
+    if (turn) x = rotated(a.pairs, x, y, g);
+    // (a row's lanes are of one wave and load before they store, so q_out may be q)
+    *((uint4*)(to + h * a.q_out.head) + piece) = x;
+    h += kHeads;
+    if (h >= a.Hq) break;
+    x = *((const uint4*)(from + h * a.q.head) + piece);
+    y = *((const uint4*)(from + h * a.q.head) + other);
   }
 }
 
-template <int D, bool LOAD>
-__global__ __launch_bounds__(kRowsThreads) void k_cache_write(CacheWriteArgs a, int kv_units) {
+template <int D, bool LOAD, int T>
+__global__ __launch_bounds__(T) void k_cache_write(CacheWriteArgs a, int kv_units) {
   using B = CacheBlock<D>;
   constexpr int LPT = D / 8;                         // lanes of a row
-  constexpr int kPasses = kCacheBlock * LPT / kRowsThreads;
-  __shared__ QuantTables tab;
+  constexpr int kPasses = kCacheBlock * LPT / T;
   __shared__ uint32_t codes[kCacheBlock][LPT + 1];   // value codes, element i in nibble i
-  __shared__ uint32_t written;                       // the block's tokens that are written
+  __shared__ uint4 words[D];                         // the block's value words
   if (!LOAD && (int)blockIdx.x >= kv_units) {
-    rotate_queries<D>(a, (int)blockIdx.x - kv_units);
+    rotate_queries<D, T>(a, (int)blockIdx.x - kv_units);
     return;
   }
-  const int heads = a.c.L * a.c.Hkv;
-  const int lh = (int)blockIdx.x % heads, rest = (int)blockIdx.x / heads;
-  const int layer = lh / a.c.Hkv, head = lh % a.c.Hkv;
+  const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest);
+  const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
   int b, j, len;
   int64_t row0;  // the source row of the sequence's token 0 (may be before the source's start)
   int start;     // the first token written
@@ -172,83 +299,109 @@ __global__ __launch_bounds__(kRowsThreads) void k_cache_write(CacheWriteArgs a, 
     start = 0;
     len = (int)(a.kept_off[b + 1] - row0);
   } else {
-    b = rest / a.blocks;
+    b = a.by_blocks.div(rest);
     const StepSeq q = step_sequence(a.c, a.s, b);
     len = q.count == 0 ? 0 : q.len;
     row0 = (int64_t)q.row - (q.len - q.count);
     start = max(q.len - q.count, 0);
-    j = (start >> 5) + rest % a.blocks;
+    j = (start >> 5) + a.by_blocks.mod(rest, b);
   }
   if (j * kCacheBlock >= len) return;
-  uint8_t* blk = cache_block<D>(a.c, layer, head, b, j);
-  if (blk == nullptr) return;
-  if (!LOAD) build_tables(tab, 7.0f, a.ro.off);
-  if (threadIdx.x < 64) {
-    const int t = j * kCacheBlock + (int)threadIdx.x;
-    bool w = threadIdx.x < kCacheBlock && t >= start && t < len;
-    if (!LOAD && w && a.cos_sin != nullptr) {
-      const int64_t pos = a.positions[row0 + t];
-      w = pos >= 0 && pos < a.num_positions;
-    }
-    const uint32_t m = (uint32_t)__builtin_amdgcn_ballot_w64(w);
-    if (threadIdx.x == 0) written = m;
-  }
-  __syncthreads();
-  const uint32_t mask = written;
+  const int32_t page = scalar_load(a.c.table + (int64_t)b * a.c.max_pages + (j >> a.c.page_shift));
+  const bool turned = !LOAD && a.cos_sin != nullptr;
   const int piece = threadIdx.x % LPT;
+  const bool turn = turned && rotates(a, piece);
+  const int other = turn && !a.pairs ? partner(a, piece) : piece;
+
+  // the lane's pieces of its rows
+  uint4 kx[kPasses], ky[kPasses], vx[kPasses];
+  uint32_t vc[kPasses];
+  float gamma[kPasses];
+  int64_t pos[kPasses];
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
-    const int slot = (int)threadIdx.x / LPT + p * (kRowsThreads / LPT);
+    const int token = j * kCacheBlock + p * (T / LPT) + (int)threadIdx.x / LPT;
+    const int64_t row = row0 + token;
+    kx[p] = ky[p] = vx[p] = make_uint4(0, 0, 0, 0);
+    vc[p] = 0;
+    gamma[p] = 0.0f;
+    pos[p] = 0;
+    if (token < start || token >= len) continue;
+    const uint16_t* k = a.k.data + layer * a.k.layer + row * a.k.token + head * a.k.head;
+    if (turned) pos[p] = a.positions[row];
+    kx[p] = *((const uint4*)k + piece);
+    if (turned) ky[p] = *((const uint4*)k + other);
+    if (LOAD) {
+      const int64_t at = (int64_t)lh * a.kept_off[a.c.batch] + row;
+      vc[p] = *((const uint32_t*)(a.v_q + at * (D / 2)) + piece);
+      gamma[p] = a.v_scales[at];
+    } else {
+      vx[p] = *((const uint4*)(a.v.data + layer * a.v.layer + row * a.v.token + head * a.v.head) + piece);
+    }
+  }
+  // the tokens that are written, the same in every wave
+  uint32_t mask;
+  {
+    const int t = j * kCacheBlock + (int)(threadIdx.x & 63);
+    bool in = (threadIdx.x & 63) < kCacheBlock && t >= start && t < len;
+    if (turned && in) {
+      const int64_t at = a.positions[row0 + t];
+      in = at >= 0 && at < a.num_positions;
+    }
+    mask = (uint32_t)__builtin_amdgcn_ballot_w64(in);
+  }
+  if (page < 0 || page >= a.c.num_pages || mask == 0) return;
+  uint8_t* blk = a.c.pages + ((((((int64_t)layer * a.c.num_pages + page) * a.c.Hkv + head) << a.c.page_shift) +
+                               (j & ((1 << a.c.page_shift) - 1))) * B::kBytes);
+  uint4* out = (uint4*)(blk + B::kValues) + threadIdx.x;
+  uint4 old = make_uint4(0, 0, 0, 0);
+  if (mask != 0xFFFFFFFFu && threadIdx.x < D) old = *out;
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p) {
+    const int slot = p * (T / LPT) + (int)threadIdx.x / LPT;
     const bool w = (mask >> slot) & 1u;
-    const int64_t row = row0 + j * kCacheBlock + slot;
-    uint4 kx = make_uint4(0, 0, 0, 0);
-    if (w) {
-      const uint16_t* k = a.k.data + layer * a.k.layer + row * a.k.token + head * a.k.head;
-      if (!LOAD && a.cos_sin != nullptr)
-        kx = rotated_piece(a, k, piece, a.cos_sin + (int64_t)a.positions[row] * a.rotary_dim);
-      else
-        kx = *((const uint4*)k + piece);
+    if (__builtin_amdgcn_ballot_w64(w) == 0) continue;  // a wave without a token has nothing to quantise
+    if (turned) {
+      Angles g = {};
+      if (turn && w) g = load_angles(a, a.cos_sin + pos[p] * a.rotary_dim, piece);
+      const uint4 r = rotated(a.pairs, kx[p], ky[p], g);
+      if (turn && w) kx[p] = r;
     }
     uint32_t scale;
-    const uint32_t word = key_codes(kx, scale);  // every lane takes part
+    const uint32_t word = key_codes(kx[p], scale);  // every lane takes part
+    if (!LOAD) vc[p] = value_codes<LPT>(vx[p], gamma[p]);
+    codes[slot][piece] = vc[p];
     if (w) {
       *((uint32_t*)(blk + B::kKeys) + slot * LPT + (piece & 3) * (D / 32) + (piece >> 2)) = word;
       if ((piece & 3) == 0) *((uint16_t*)(blk + B::kKeyScales) + slot * (D / 32) + (piece >> 2)) = (uint16_t)scale;
-    }
-    if (LOAD) {
-      const int64_t at = (int64_t)lh * a.kept_off[a.c.batch] + row;
-      if (w) {
-        codes[slot][piece] = *((const uint32_t*)(a.v_q + at * (D / 2)) + piece);
-        if (piece == 0) *((float*)(blk + B::kValueScales) + slot) = a.v_scales[at];
-      }
-    } else {
-      const uint4 vx = w ? *((const uint4*)(a.v.data + layer * a.v.layer + row * a.v.token + head * a.v.head) + piece)
-                         : make_uint4(0, 0, 0, 0);
-      const QuantFmt f{true, true, 7.0f};
-      uint2 c;
-      const float gamma = quant_piece<LPT, kQNibble>(vx, tab, f, c);
-      codes[slot][piece] = c.x;
-      if (w && piece == 0) *((float*)(blk + B::kValueScales) + slot) = gamma;
+      if (piece == 0) *((float*)(blk + B::kValueScales) + slot) = gamma[p];
     }
   }
   __syncthreads();
-  // the value words: channel x of eight tokens
-  for (int i = threadIdx.x; i < 4 * D; i += kRowsThreads) {
-    const int lane = (i & 255) >> 2, g = lane >> 4;
-    const int x = (i >> 8) * 64 + (i & 3) * 16 + (lane & 15);
-    uint32_t set = 0, word = 0;
+  if (threadIdx.x < 4 * LPT) {  // the tokens of a group g, eight channels
+    const int g = threadIdx.x / LPT, c8 = threadIdx.x % LPT;
+    uint32_t in[8], tr[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int slot = (e >> 2) * 16 + 4 * g + (e & 3);
-      if ((mask >> slot) & 1u) {
-        set |= 0xFu << (4 * nibble_of(e));
-        // two's complement to c + 8: the sign bit flipped
-        word |= (((codes[slot][x >> 3] >> (4 * (x & 7))) ^ 8u) & 0xFu) << (4 * nibble_of(e));
-      }
-    }
-    uint32_t* to = (uint32_t*)(blk + B::kValues) + i;
-    if (set == 0) continue;
-    *to = set == 0xFFFFFFFFu ? word : ((*to & ~set) | word);
+    for (int e = 0; e < 8; ++e) in[e] = codes[(e >> 2) * 16 + 4 * g + (e & 3)][c8];
+    transpose(in, tr);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)  // two's complement to c + 8: the sign bits flipped
+      ((uint32_t*)words)[(c8 >> 3) * 256 + (16 * g + (c8 & 1) * 8 + i) * 4 + ((c8 >> 1) & 3)] = tr[i] ^ 0x88888888u;
+  }
+  __syncthreads();
+  if (threadIdx.x < D) {
+    const int g = (threadIdx.x & 63) >> 4;
+    uint32_t set = 0;  // the nibbles of the tokens that are written
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if ((mask >> ((e >> 2) * 16 + 4 * g + (e & 3))) & 1u) set |= 0xFu << (4 * nibble_of(e));
+    if (set == 0) return;
+    uint4 x = words[threadIdx.x];
+    x.x = (old.x & ~set) | (x.x & set);
+    x.y = (old.y & ~set) | (x.y & set);
+    x.z = (old.z & ~set) | (x.z & set);
+    x.w = (old.w & ~set) | (x.w & set);
+    *out = x;
   }
 }
 
@@ -266,43 +419,49 @@ __device__ inline uint4 held_row(const float (&c)[8], float scale) {
 template <int D>
 __global__ __launch_bounds__(kRowsThreads) void k_cache_read(CacheReadArgs a) {
   using B = CacheBlock<D>;
-  constexpr int LPT = D / 8;
-  constexpr int kPasses = kCacheBlock * LPT / kRowsThreads;
-  __shared__ uint32_t words[4 * D];
-  const int heads = a.c.L * a.c.Hkv;
-  const int lh = (int)blockIdx.x % heads, b = blockIdx.y;
+  constexpr int LPT = D / 8, kPasses = kCacheBlock * LPT / kRowsThreads;
+  __shared__ uint4 words[D];
+  const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest), b = blockIdx.y;
+  const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
   const int64_t first = a.first[b], n = a.off[b + 1] - a.off[b];
-  const int64_t j = (first >> 5) + (int)blockIdx.x / heads;
+  const int64_t j = (first >> 5) + rest;
   if (j * kCacheBlock >= first + n) return;
-  const int32_t raw = a.c.lens[b];
+  const int32_t raw = scalar_load(a.c.lens + b);
   const int32_t len = raw < 0 || raw > a.c.max_len ? 0 : raw;
-  const uint8_t* blk = j * kCacheBlock < len ? cache_block<D>(a.c, lh / a.c.Hkv, lh % a.c.Hkv, b, (int)j) : nullptr;
-  if (blk != nullptr)
-    for (int i = threadIdx.x; i < D; i += kRowsThreads)
-      *((uint4*)words + i) = *((const uint4*)(blk + B::kValues) + i);
-  __syncthreads();
+  const uint8_t* blk = j * kCacheBlock < len ? cache_block<D>(a.c, layer, head, b, (int)j) : nullptr;
   const int piece = threadIdx.x % LPT;
+  uint32_t kw[kPasses], ks[kPasses];
+  float vs[kPasses];
+  if (blk != nullptr) {
+    if (threadIdx.x < D) words[threadIdx.x] = *((const uint4*)(blk + B::kValues) + threadIdx.x);
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      const int slot = p * (kRowsThreads / LPT) + (int)threadIdx.x / LPT;
+      kw[p] = *((const uint32_t*)(blk + B::kKeys) + slot * LPT + (piece & 3) * (D / 32) + (piece >> 2));
+      ks[p] = *((const uint16_t*)(blk + B::kKeyScales) + slot * (D / 32) + (piece >> 2));
+      vs[p] = *((const float*)(blk + B::kValueScales) + slot);
+    }
+  }
+  __syncthreads();
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
-    const int slot = (int)threadIdx.x / LPT + p * (kRowsThreads / LPT);
+    const int slot = p * (kRowsThreads / LPT) + (int)threadIdx.x / LPT;
     const int64_t t = j * kCacheBlock + slot;
     if (t < first || t >= first + n) continue;
     uint4 k = make_uint4(0, 0, 0, 0), v = k;
     if (blk != nullptr && t < len) {
-      const uint32_t w = *((const uint32_t*)(blk + B::kKeys) + slot * LPT + (piece & 3) * (D / 32) + (piece >> 2));
-      const uint32_t ks = *((const uint16_t*)(blk + B::kKeyScales) + slot * (D / 32) + (piece >> 2));
       float c[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = (float)((int)((w >> (4 * nibble_of(e))) & 0xFu) - 8);
-      k = held_row(c, __uint_as_float(ks << 16));
-      const int g = (slot >> 2) & 3, e = (slot >> 4) * 4 + (slot & 3);
+      for (int e = 0; e < 8; ++e) c[e] = (float)((int)((kw[p] >> (4 * nibble_of(e))) & 0xFu) - 8);
+      k = held_row(c, __uint_as_float(ks[p] << 16));
+      const int g = (slot >> 2) & 3, shift = 4 * nibble_of((slot >> 4) * 4 + (slot & 3));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int x = piece * 8 + i;
-        const uint32_t vw = words[(x >> 6) * 256 + (g * 16 + (x & 15)) * 4 + ((x >> 4) & 3)];
-        c[i] = (float)((int)((vw >> (4 * nibble_of(e))) & 0xFu) - 8);
+        const uint32_t vw = ((const uint32_t*)words)[(x >> 6) * 256 + (g * 16 + (x & 15)) * 4 + ((x >> 4) & 3)];
+        c[i] = (float)((int)((vw >> shift) & 0xFu) - 8);
       }
-      v = held_row(c, *((const float*)(blk + B::kValueScales) + slot));
+      v = held_row(c, vs[p]);
     }
     const int64_t to = (int64_t)lh * a.off[a.c.batch] + a.off[b] + (t - first);
     *((uint4*)(a.k + to * D) + piece) = k;
@@ -310,30 +469,44 @@ __global__ __launch_bounds__(kRowsThreads) void k_cache_read(CacheReadArgs a) {
   }
 }
 
+// Divisors of the workgroups' numbers.
+template <typename Args>
+void set_heads(Args& a) {
+  a.heads = Divisor::of((int64_t)a.c.L * a.c.Hkv);
+  a.by_Hkv = Divisor::of(a.c.Hkv);
+}
+
 }  // namespace
 
-hipError_t launch_cache_append(const CacheWriteArgs& a, int head_dim, hipStream_t stream) {
+hipError_t launch_cache_append(CacheWriteArgs& a, int head_dim, hipStream_t stream) {
   const int units = a.c.L * a.c.Hkv * a.blocks * a.c.batch;
-  const unsigned grid = (unsigned)units + (a.q.data != nullptr ? (unsigned)(a.c.L * a.s.total) : 0u);
-  if (head_dim == 128)
-    hipLaunchKernelGGL((k_cache_write<128, false>), dim3(grid), dim3(kRowsThreads), 0, stream, a, units);
+  set_heads(a);
+  a.by_blocks = Divisor::of(a.blocks);
+  a.by_total = Divisor::of(a.s.total);
+  const dim3 grid((unsigned)units + (a.q.data != nullptr ? (unsigned)(a.c.L * a.s.total) : 0u));
+  if (head_dim == 128 && a.s.max_new <= kFewTokens)
+    hipLaunchKernelGGL((k_cache_write<128, false, kFewThreads>), grid, dim3(kFewThreads), 0, stream, a, units);
+  else if (head_dim == 128)
+    hipLaunchKernelGGL((k_cache_write<128, false, kRowsThreads>), grid, dim3(kRowsThreads), 0, stream, a, units);
   else
-    hipLaunchKernelGGL((k_cache_write<64, false>), dim3(grid), dim3(kRowsThreads), 0, stream, a, units);
+    hipLaunchKernelGGL((k_cache_write<64, false, kRowsThreads>), grid, dim3(kRowsThreads), 0, stream, a, units);
   return hipGetLastError();
 }
 
-hipError_t launch_cache_load(const CacheWriteArgs& a, int head_dim, hipStream_t stream) {
+hipError_t launch_cache_load(CacheWriteArgs& a, int head_dim, hipStream_t stream) {
   const int units = a.c.L * a.c.Hkv * a.blocks;
   const dim3 grid((unsigned)units, (unsigned)a.c.batch);
+  set_heads(a);
   if (head_dim == 128)
-    hipLaunchKernelGGL((k_cache_write<128, true>), grid, dim3(kRowsThreads), 0, stream, a, units);
+    hipLaunchKernelGGL((k_cache_write<128, true, kRowsThreads>), grid, dim3(kRowsThreads), 0, stream, a, units);
   else
-    hipLaunchKernelGGL((k_cache_write<64, true>), grid, dim3(kRowsThreads), 0, stream, a, units);
+    hipLaunchKernelGGL((k_cache_write<64, true, kRowsThreads>), grid, dim3(kRowsThreads), 0, stream, a, units);
   return hipGetLastError();
 }
 
-hipError_t launch_cache_read(const CacheReadArgs& a, int head_dim, hipStream_t stream) {
+hipError_t launch_cache_read(CacheReadArgs& a, int head_dim, hipStream_t stream) {
   const dim3 grid((unsigned)(a.c.L * a.c.Hkv * a.blocks), (unsigned)a.c.batch);
+  set_heads(a);
   if (head_dim == 128)
     hipLaunchKernelGGL(k_cache_read<128>, grid, dim3(kRowsThreads), 0, stream, a);
   else
