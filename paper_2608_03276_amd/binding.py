@@ -503,7 +503,7 @@ class Cache:
         if _nbytes(pages) == 0 or _nbytes(pages) % each:
             raise ValueError(f"pages holds {_nbytes(pages)} bytes, needs a multiple of {each}")
         self.pages, self.page_table, self.lens, self.device = pages, page_table, lens, pages.device
-        self.dims = (d.num_layers, d.num_q_heads, d.num_kv_heads, d.head_dim)
+        self.dims, self.index = bytes(d), pages.get_device()
         self.batch, self.page_tokens = page_table.shape[0], int(page_tokens)
         self.c = TpCache(pages.data_ptr(), page_table.data_ptr(), None if lens is None else lens.data_ptr(),
                          _nbytes(pages) // each, int(page_tokens), page_table.shape[1], page_table.shape[0])
@@ -518,6 +518,7 @@ class Step:
         if offsets is not None:
             _device_tensor(offsets, torch.int32, "offsets")
         self.offsets, self.total, self.max_new = offsets, int(total), int(max_new)
+        self.batch = None if offsets is None else offsets.numel() - 1
         self.c = TpStep(None if offsets is None else offsets.data_ptr(), self.total, self.max_new)
         self.ref = ctypes.byref(self.c)
 
@@ -534,37 +535,38 @@ class Rope:
         self.ref = ctypes.byref(self.c)
 
 
-def _rows(t, d: TpDims, heads: int, step: Step, name: str):
+def _rows(t, layers: int, total: int, heads: int, head_dim: int, name: str):
     """tp_rows of a bf16 tensor [total][heads][d] (one layer) or [L][total][heads][d] at any strides; a
     head-major tensor is given as its permuted view."""
-    if not t.is_cuda or t.dtype != torch.bfloat16:
+    shape, strides = t.shape, t.stride()
+    if t.dtype is not torch.bfloat16:
         raise ValueError(f"{name} must be a device tensor of torch.bfloat16")
-    shape, strides = tuple(t.shape), t.stride()
-    if len(shape) == 3:
-        shape, strides = (1, *shape), (0, *strides)
-    if shape != (d.num_layers, step.total, heads, d.head_dim):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, needs "
-                         f"{(d.num_layers, step.total, heads, d.head_dim)} ([L][total][heads][d])")
-    if strides[3] != 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
-    return TpRows(t.data_ptr(), *strides[:3])
+    if layers == 1 and len(shape) == 3:
+        if shape[0] == total and shape[1] == heads and shape[2] == head_dim and strides[2] == 1:
+            return TpRows(t.data_ptr(), 0, strides[0], strides[1])
+    elif tuple(shape) == (layers, total, heads, head_dim) and strides[3] == 1:
+        return TpRows(t.data_ptr(), *strides[:3])
+    raise ValueError(f"{name} has shape {tuple(shape)}, strides {tuple(strides)}; needs "
+                     f"{(layers, total, heads, head_dim)} ([L][total][heads][d]), the last dimension contiguous")
 
 
 def _cache_call(d: TpDims, cache: Cache, tensors, stream):
-    """The stream of a call (the current one of the cache's device), after the checks all calls share."""
-    if (d.num_layers, d.num_q_heads, d.num_kv_heads, d.head_dim) != cache.dims:
+    """The stream of a call (the current one of the cache's device), after the checks all calls share.  Kept lean: a
+    decode step makes these calls for every layer."""
+    if bytes(d) != cache.dims:
         raise ValueError("the cache was made for other dims")
+    index = cache.index
     for t in tensors:
-        if t is not None and t.device != cache.device:
+        if t is not None and t.get_device() != index:
             raise ValueError(f"a tensor on {t.device} for a cache on {cache.device}")
     if stream is None:
-        return torch.cuda.current_stream(cache.device).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(index)
     return _stream(stream)
 
 
 def _need_step(cache: Cache, step: Step):
-    if step.offsets is not None and step.offsets.numel() != cache.batch + 1:
-        raise ValueError(f"offsets holds {step.offsets.numel()} entries, needs {cache.batch + 1}")
+    if step.offsets is not None and step.batch != cache.batch:
+        raise ValueError(f"offsets holds {step.batch + 1} entries, needs {cache.batch + 1}")
 
 
 def tp_cache_page_bytes(d: TpDims, page_tokens: int) -> int:
@@ -594,16 +596,15 @@ def tp_cache_append(d: TpDims, cache: Cache, step: Step, k, v, positions=None, r
     into q_out.  k, v [total][Hkv][d], q, q_out [total][Hq][d] (or with a leading [L]), any strides."""
     s = _cache_call(d, cache, (k, v, positions, q, q_out, step.offsets, None if rope is None else rope.cos_sin), stream)
     _need_step(cache, step)
-    rk, rv = _rows(k, d, d.num_kv_heads, step, "k"), _rows(v, d, d.num_kv_heads, step, "v")
-    rq = ro = None
-    if q is not None:
-        rq = ctypes.byref(_rows(q, d, d.num_q_heads, step, "q"))
-    if q_out is not None:
-        ro = ctypes.byref(_rows(q_out, d, d.num_q_heads, step, "q_out"))
+    L, Hq, Hkv, D, n = d.num_layers, d.num_q_heads, d.num_kv_heads, d.head_dim, step.total
+    byref = ctypes.byref
+    rq = None if q is None else byref(_rows(q, L, n, Hq, D, "q"))
+    ro = None if q_out is None else byref(_rows(q_out, L, n, Hq, D, "q_out"))
     if positions is not None:
-        _device_tensor(positions, torch.int32, "positions", (step.total,))
-    _check(load().tp_cache_append(ctypes.byref(d), cache.ref, step.ref, ctypes.byref(rk), ctypes.byref(rv),
-                                  _ptr(positions), None if rope is None else rope.ref, rq, ro, s))
+        _device_tensor(positions, torch.int32, "positions", (n,))
+    _check(load().tp_cache_append(byref(d), cache.ref, step.ref, byref(_rows(k, L, n, Hkv, D, "k")),
+                                  byref(_rows(v, L, n, Hkv, D, "v")), _ptr(positions),
+                                  None if rope is None else rope.ref, rq, ro, s))
 
 
 def tp_cache_workspace_size(d: TpDims, cache: Cache, step: Step, max_len: int) -> int:
@@ -618,15 +619,17 @@ def tp_cache_attention(d: TpDims, cache: Cache, step: Step, q, softmax_scale: fl
     (natural log) or None."""
     s = _cache_call(d, cache, (q, o, lse, workspace, step.offsets), stream)
     _need_step(cache, step)
-    rq, ro = _rows(q, d, d.num_q_heads, step, "q"), _rows(o, d, d.num_q_heads, step, "o")
+    L, Hq, D, n = d.num_layers, d.num_q_heads, d.head_dim, step.total
+    byref = ctypes.byref
     if lse is not None:
-        _need(lse, d.num_layers * d.num_q_heads * step.total * 4, "lse")
+        _need(lse, L * Hq * n * 4, "lse")
     if workspace is None:
         workspace = torch.empty(tp_cache_workspace_size(d, cache, step, max_len), dtype=torch.uint8, device=cache.device)
         if stream is not None:  # allocated on the current stream: kept until the work on the other one is done
             workspace.record_stream(torch.cuda.ExternalStream(s, device=cache.device))
-    _check(load().tp_cache_attention(ctypes.byref(d), cache.ref, step.ref, ctypes.byref(rq), float(softmax_scale),
-                                     int(max_len), ctypes.byref(ro), _ptr(lse), _ptr(workspace), _nbytes(workspace), s))
+    _check(load().tp_cache_attention(byref(d), cache.ref, step.ref, byref(_rows(q, L, n, Hq, D, "q")), softmax_scale,
+                                     max_len, byref(_rows(o, L, n, Hq, D, "o")), _ptr(lse), workspace.data_ptr(),
+                                     _nbytes(workspace), s))
 
 
 def tp_cache_read(d: TpDims, cache: Cache, batch: Batch, k_out, v_out, first=None, stream=None):

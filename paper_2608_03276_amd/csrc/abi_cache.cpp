@@ -254,6 +254,7 @@ static tp_status prepare_attention(const tp_dims* dims, const tp_cache* cache, c
   a.row_groups = plan.row_groups;
   a.chunk = plan.chunk;
   a.chunks = plan.chunks;
+  a.waves = plan.waves;
   a.once = plan.once;
   return TP_OK;
 }

@@ -33,8 +33,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int W = 4;  // waves of a workgroup
-constexpr int kAttnThreads = 64 * W, kMergeThreads = 256;
+constexpr int kMergeThreads = 256;
 constexpr float kNoMax = -3.402823466e38f;  // (maximum, sum) of nothing is (kNoMax, 0): joining it changes nothing
 constexpr float kLn2 = 0.6931471805599453f;
 // A row's reference is set so that its largest weight is 2^kSet, and raised when one exceeds 2^kLimit (fp16
@@ -149,9 +148,9 @@ __device__ inline void store_output(const CacheAttnArgs& a, int layer, int64_t t
         st.y > 0.0f ? (st.x + __builtin_amdgcn_logf(st.y)) * kLn2 : -INFINITY;
 }
 
-// NR tiles of 16 rows.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave it out).
-template <int D, int NR, bool ONCE>
-__global__ __launch_bounds__(kAttnThreads, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache_attention(CacheAttnArgs a) {
+// NR tiles of 16 rows, W waves.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave it out).
+template <int D, int NR, int W, bool ONCE>
+__global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache_attention(CacheAttnArgs a) {
   using B = CacheBlock<D>;
   constexpr int KS = D / 32;  // products of a score: channels in steps of 32
   constexpr int ND = D / 16;  // output tiles: channels in steps of 16
@@ -512,10 +511,12 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache_merge(CacheAttnArgs a) 
 //    occupy every CU (32 sequences of 8 heads and 2049 to 2548 tokens: 27.2 us whole, 29.9 in chunks of 640);
 //    otherwise about 1024 workgroups, in chunks of 512 at least (one sequence of 13215, 8 heads: 11.1 us at 512, 13.5
 //    at 1024, 25.9 at 4096; two of 262144 and 131073: 78.0 us at 4096, 92.1 at 1024, 94.1 at 8192).
+//    Whole sequences of at most two workgroups a CU take eight waves (those 32 sequences: 26.2 us with four, 23.4
+//    with eight, the append before it 5.8 of them; 64 of 6K to 32K tokens in chunks: 235 and 249).
 //  - Four tiles (prompts): whole sequences from 1024 workgroups on, fewer are brought to that number.
 CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
                      int32_t max_len) {
-  constexpr int64_t kUnit = 32 * W;  // tokens: a block for each wave
+  constexpr int64_t kUnit = 128;  // tokens: a block for each of four waves
   constexpr int64_t kLeast = 512, kWhole = 4096, kWorkgroups = 1024, kCus = 256;
   CachePlan p;
   const int64_t rows = (int64_t)(Hq / Hkv) * max_new;
@@ -530,6 +531,7 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
   // Partial rows: up to 32 a pair in chunks of kWhole, up to 64 (kWorkgroups + units) in the fill.  The bound
   // grows with every argument, so a buffer for the longest call serves the others.
   const int64_t partials = finest == 1 ? 0 : std::min(heads * rows * finest, 128 * kWorkgroups + 32 * heads * whole);
+  p.waves = p.tiles == 1 && p.chunks == 1 && units <= 2 * kCus ? 8 : 4;
   p.once = p.row_groups == 1 &&
            (double)heads * max_len * (double)(cache_block_bytes(head_dim) / kCacheBlock) > (double)(256 << 20);
   p.stat_off = 0;
@@ -540,21 +542,22 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
 
 namespace {
 
-template <int D, int NR>
+template <int D, int NR, int W>
 void launch_part(const CacheAttnArgs& a, dim3 grid, hipStream_t stream) {
   if (a.once)
-    hipLaunchKernelGGL((k_cache_attention<D, NR, true>), grid, dim3(kAttnThreads), 0, stream, a);
+    hipLaunchKernelGGL((k_cache_attention<D, NR, W, true>), grid, dim3(64 * W), 0, stream, a);
   else
-    hipLaunchKernelGGL((k_cache_attention<D, NR, false>), grid, dim3(kAttnThreads), 0, stream, a);
+    hipLaunchKernelGGL((k_cache_attention<D, NR, W, false>), grid, dim3(64 * W), 0, stream, a);
 }
 
 template <int D>
 hipError_t launch_attention(const CacheAttnArgs& a, hipStream_t stream) {
   const unsigned heads = (unsigned)(a.c.L * a.c.Hkv), batch = (unsigned)a.c.batch;
   const dim3 grid(heads * a.row_groups * a.chunks, batch);
-  if (a.tiles == 1) launch_part<D, 1>(a, grid, stream);
-  else if (a.tiles == 2) launch_part<D, 2>(a, grid, stream);
-  else launch_part<D, 4>(a, grid, stream);
+  if (a.tiles == 1 && a.waves == 8) launch_part<D, 1, 8>(a, grid, stream);
+  else if (a.tiles == 1) launch_part<D, 1, 4>(a, grid, stream);
+  else if (a.tiles == 2) launch_part<D, 2, 4>(a, grid, stream);
+  else launch_part<D, 4, 4>(a, grid, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.chunks == 1) return e;
   const unsigned rows = heads * a.row_groups * a.tiles * 16;  // 16 a tile

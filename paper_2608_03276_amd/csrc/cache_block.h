@@ -138,6 +138,7 @@ hipError_t launch_cache_read(CacheReadArgs& a, int head_dim, hipStream_t stream)
 // 128), whose partial results are merged when there are several.
 struct CachePlan {
   int32_t tiles, row_groups, chunk, chunks;
+  int32_t waves; // of a workgroup
   int32_t once;  // whether the loads leave the caches alone: the cache is read once a call, and no call finds it there
   size_t stat_off, o_off, total;  // workspace: (max, sum) float2 and output fp32 [D] of each row and chunk
 };
@@ -155,7 +156,7 @@ struct CacheAttnArgs {
   Divisor R;        // query heads of a KV head
   Divisor heads, by_Hkv, by_groups, by_chunk;  // L * Hkv, Hkv, row_groups, chunk
   float scale_log2; // softmax_scale * log2(e)
-  int32_t tiles, row_groups, chunk, chunks, once;
+  int32_t tiles, row_groups, chunk, chunks, waves, once;
 };
 hipError_t launch_cache_attention(const CacheAttnArgs& a, int head_dim, hipStream_t stream);
 
