@@ -45,8 +45,10 @@ constexpr float kSet = 8.0f, kLimit = 16384.0f;
 constexpr float kLeastScale = 0x1p-60f;
 
 // Key scales as fp16 numbers: the largest of a block is set to exponent field 24 (2^9), and the setting is kept
-// while the largest of a block has field 14 to 27 (a code times a scale stays below 2^16).
-constexpr int kScaleSet = 24, kScaleLow = 14 << 7, kScaleHigh = 28 << 7;
+// while the largest of a block has field 20 to 27 (a code times a scale stays below 2^16).  A code times a scale
+// is exact, 3 by 8 bits in fp16's 11, down to field 1: a scale 2^19 or more below the largest of its block counts as
+// zero or one off by less than 2^-19 of that.
+constexpr int kScaleSet = 24, kScaleLow = 20 << 7, kScaleHigh = 28 << 7;
 
 union Frag {
   uint32_t w[4];
