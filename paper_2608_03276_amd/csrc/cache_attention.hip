@@ -525,11 +525,11 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
   p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   p.row_groups = (int32_t)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
   const int64_t heads = (int64_t)L * Hkv * batch, units = heads * p.row_groups;
-  const int64_t finest = (max_len + kLeast - 1) / kLeast, whole = (max_len + kWhole - 1) / kWhole;
+  const int64_t n = max_len, finest = (n + kLeast - 1) / kLeast, whole = (n + kWhole - 1) / kWhole;
   const int64_t fill = std::min(finest, (kWorkgroups + units - 1) / units);
   int64_t chunks = p.tiles == 4 ? fill : units >= kCus ? whole : std::max(whole, fill);
-  p.chunk = (int32_t)(((max_len + chunks - 1) / chunks + kUnit - 1) / kUnit * kUnit);
-  p.chunks = (int32_t)((max_len + p.chunk - 1) / p.chunk);
+  p.chunk = (int32_t)(((n + chunks - 1) / chunks + kUnit - 1) / kUnit * kUnit);
+  p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
   // Partial rows: up to 32 a pair in chunks of kWhole, up to 64 (kWorkgroups + units) in the fill.  The bound
   // grows with every argument, so a buffer for the longest call serves the others.
   const int64_t partials = finest == 1 ? 0 : std::min(heads * rows * finest, 128 * kWorkgroups + 32 * heads * whole);
