@@ -292,6 +292,8 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
     load_keys(blk);
     load_values(blk);
   }
+  // the group's tiles: a decoding sequence beside a prompt's chunk has one, whose weights alone are formed
+  const int tiles = (rg.rows - rg.row0 + 15) / 16;
   int bias = 0;  // bf16 bits taken off a key scale: it becomes an fp16 number times 2^(bias / 128 - 112)
   for (int j = j0; j < j1; j += W) {
     const bool missing = page_of(j) < 0;
@@ -341,9 +343,10 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
     __builtin_amdgcn_sched_barrier(0);
     load_keys(next);
 
-    Frag pf[NR];
+    Frag pf[NR] = {};
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
+      if (r > 0 && r >= tiles) break;
       float w[8], p[8], sum, top;
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = __uint_as_float(vs[i >> 2][i & 3]);
@@ -405,6 +408,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
+    if (r > 0 && r >= tiles) break;
     float top = kNoMax;
 #pragma unroll
     for (int w = 0; w < W; ++w) top = fmaxf(top, lds_stat[w][r * 16 + n].x);
