@@ -457,13 +457,14 @@ tp_status tp_cache_load(const tp_dims* dims, const tp_cache* cache, const int64_
  *   key   token t of sequence b is written from k's row offsets[b] + t, rotated at positions[row];
  *   value from v's row;
  *   q_out[row] = q[row] rotated, for every row of a sequence; q_out may be q (the same data and strides).
- * The rotation's products and sums are formed in 64 bits and rounded to bf16 once (nearest even; beyond the
- * largest finite value to that value); the key's codes are formed from the rounded row.
+ * The rotation's products and sums are formed in 64 bits and rounded to fp32, then to bf16 (nearest even;
+ * beyond the largest finite value to that value); the key's codes are formed from the rounded row.
  * positions: device int32 [total]; a row whose position is outside [0, num_positions) is not written
  * (neither key, value nor q_out).  rope NULL: no rotation, positions unused (may be NULL), q and
  * q_out NULL.  q and q_out are given together.
  * k, v rows of Hkv heads, q, q_out of Hq.  New tokens that lie before the sequence's start
- * (lens[b] < T_b) are not written.  A page that two sequences share may be written by neither.
+ * (lens[b] < T_b) are not written.  A page that the table lists twice (a prefix that sequences share) may
+ * not be written.
  * Inputs are finite.
  * Errors: TP_ERR_NULL, TP_ERR_SHAPE, TP_ERR_PARAM, TP_ERR_UNSUPPORTED, TP_ERR_HIP.
  */
@@ -498,7 +499,7 @@ tp_status tp_cache_attention(const tp_dims* dims, const tp_cache* cache, const t
 /*
  * Ranges of the sequences back as bf16 rows, the layout the eviction takes (a long answer is evicted
  * again): for t < n_b = ctx_offsets[b + 1] - ctx_offsets[b] and p = first[b] + t,
- *   k_out[l][h][ctx_offsets[b] + t][:] = bf16(key held of token p),  v_out likewise,
+ *   k_out[l][h][ctx_offsets[b] + t][:] = bf16(fp32(c * scale)) of token p's key,  v_out likewise,
  * zero rows for p >= lens[b] and for tokens without a page.  batch->batch = cache->batch (so at most
  * TP_MAX_BATCH); ctx_offsets as tp_batch, but a range may be empty; guide_offsets unused.  first: host
  * [batch], >= 0, first[b] + n_b <= 2^30 (TP_ERR_SHAPE); NULL: 0.  k_out, v_out bf16 [L][Hkv][N_tot][d],

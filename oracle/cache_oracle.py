@@ -25,6 +25,11 @@ def to_bf16(x):
     return np.rint(x / unit) * unit
 
 
+def by_fp32(x):
+    """float64 -> the nearest fp32 value -> the nearest bf16 value, as float64."""
+    return to_bf16(np.clip(x, -_MAX_BF16, _MAX_BF16).astype(np.float32))
+
+
 def bf16_bits(x):
     return (np.asarray(x, dtype=np.float64).astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)
 
@@ -37,7 +42,7 @@ def rotate(x, cos_sin_row, rotary_dim, style):
         a, b = (i, i + h) if style == HALVES else (2 * i, 2 * i + 1)
         c, s = float(cos_sin_row[i]), float(cos_sin_row[h + i])
         out[a], out[b] = x[a] * c - x[b] * s, x[b] * c + x[a] * s
-    return to_bf16(out)
+    return by_fp32(out)
 
 
 def quantise_key(k):

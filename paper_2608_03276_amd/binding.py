@@ -564,6 +564,14 @@ def _cache_call(d: TpDims, cache: Cache, tensors, stream):
     return _stream(stream)
 
 
+def _on_device(cache: Cache, call, *args):
+    """The call with the cache's device current (its default stream has the handle 0 on every device)."""
+    if torch._C._cuda_getDevice() == cache.index:
+        return _check(call(*args))
+    with torch.cuda.device(cache.index):
+        return _check(call(*args))
+
+
 def _need_step(cache: Cache, step: Step):
     if step.offsets is not None and step.batch != cache.batch:
         raise ValueError(f"offsets holds {step.batch + 1} entries, needs {cache.batch + 1}")
@@ -586,8 +594,8 @@ def tp_cache_load(d: TpDims, cache: Cache, kept_offsets, k, v_q, scales, bits: i
     _need(k, n * d.head_dim * 2, "k")
     _need(v_q, n * d.head_dim // 2, "v_q")
     _need(scales, n * 4, "scales")
-    _check(load().tp_cache_load(ctypes.byref(d), cache.ref, _i64_array(kept_offsets), _ptr(k), _ptr(v_q),
-                                _ptr(scales), int(bits), s))
+    _on_device(cache, load().tp_cache_load, ctypes.byref(d), cache.ref, _i64_array(kept_offsets), _ptr(k), _ptr(v_q),
+               _ptr(scales), int(bits), s)
 
 
 def tp_cache_append(d: TpDims, cache: Cache, step: Step, k, v, positions=None, rope: Rope = None, q=None, q_out=None,
@@ -602,9 +610,8 @@ def tp_cache_append(d: TpDims, cache: Cache, step: Step, k, v, positions=None, r
     ro = None if q_out is None else byref(_rows(q_out, L, n, Hq, D, "q_out"))
     if positions is not None:
         _device_tensor(positions, torch.int32, "positions", (n,))
-    _check(load().tp_cache_append(byref(d), cache.ref, step.ref, byref(_rows(k, L, n, Hkv, D, "k")),
-                                  byref(_rows(v, L, n, Hkv, D, "v")), _ptr(positions),
-                                  None if rope is None else rope.ref, rq, ro, s))
+    _on_device(cache, load().tp_cache_append, byref(d), cache.ref, step.ref, byref(_rows(k, L, n, Hkv, D, "k")),
+               byref(_rows(v, L, n, Hkv, D, "v")), _ptr(positions), None if rope is None else rope.ref, rq, ro, s)
 
 
 def tp_cache_workspace_size(d: TpDims, cache: Cache, step: Step, max_len: int) -> int:
@@ -627,9 +634,9 @@ def tp_cache_attention(d: TpDims, cache: Cache, step: Step, q, softmax_scale: fl
         workspace = torch.empty(tp_cache_workspace_size(d, cache, step, max_len), dtype=torch.uint8, device=cache.device)
         if stream is not None:  # allocated on the current stream: kept until the work on the other one is done
             workspace.record_stream(torch.cuda.ExternalStream(s, device=cache.device))
-    _check(load().tp_cache_attention(byref(d), cache.ref, step.ref, byref(_rows(q, L, n, Hq, D, "q")), softmax_scale,
-                                     max_len, byref(_rows(o, L, n, Hq, D, "o")), _ptr(lse), workspace.data_ptr(),
-                                     _nbytes(workspace), s))
+    _on_device(cache, load().tp_cache_attention, byref(d), cache.ref, step.ref, byref(_rows(q, L, n, Hq, D, "q")),
+               softmax_scale, max_len, byref(_rows(o, L, n, Hq, D, "o")), _ptr(lse), workspace.data_ptr(),
+               _nbytes(workspace), s)
 
 
 def tp_cache_read(d: TpDims, cache: Cache, batch: Batch, k_out, v_out, first=None, stream=None):
@@ -641,5 +648,5 @@ def tp_cache_read(d: TpDims, cache: Cache, batch: Batch, k_out, v_out, first=Non
     _need(v_out, n, "v_out")
     if first is not None and len(first) != cache.batch:
         raise ValueError(f"first holds {len(first)} entries, needs {cache.batch}")
-    _check(load().tp_cache_read(ctypes.byref(d), cache.ref, ctypes.byref(batch.c),
-                                None if first is None else _i64_array(first), _ptr(k_out), _ptr(v_out), s))
+    _on_device(cache, load().tp_cache_read, ctypes.byref(d), cache.ref, ctypes.byref(batch.c),
+               None if first is None else _i64_array(first), _ptr(k_out), _ptr(v_out), s)

@@ -31,15 +31,6 @@ __device__ inline uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// f, the fp32 number next to a value that differs from it by `rest` (its sign is all that counts), as an fp32
-// number that rounds to the bf16 number the value itself rounds to: f may lie halfway between two only by its own
-// rounding.
-__device__ inline float for_bf16(float f, float rest) {
-  const uint32_t b = __float_as_uint(f);
-  if ((b & 0xFFFFu) != 0x8000u || rest == 0.0f) return f;
-  return __uint_as_float((rest > 0.0f) == ((int32_t)b >= 0) ? b + 1 : b - 1);
-}
-
 // Angles of 8 channels (of 4 pairs): cosines, and sines with the sign of the partner's term.
 struct Angles {
   float c[8], s[8];
@@ -79,19 +70,19 @@ __device__ inline Angles load_angles(const CacheWriteArgs& a, const float* cs, i
   return g;
 }
 
-// x c + y s in 64 bits (a product of a bf16 and an fp32 number is exact there), for rounding to bf16 once;
-// within its range, so that no rotation of finite rows gives an infinity.
+// x c + y s in 64 bits (a product of a bf16 and an fp32 number is exact there), as the nearest fp32 number, for
+// rounding to bf16; within its range, so that no rotation of finite rows gives an infinity.
 __device__ inline float rotated64(float x, float y, float c, float s) {
-  double r = (double)x * (double)c + (double)y * (double)s;
-  r = __builtin_fmax(__builtin_fmin(r, (double)kMaxBf16), -(double)kMaxBf16);
-  const float f = (float)r;
-  const double rest = r - (double)f;
-  return for_bf16(f, rest > 0.0 ? 1.0f : rest < 0.0 ? -1.0f : 0.0f);
+  const double r = (double)x * (double)c + (double)y * (double)s;
+  float f = (float)__builtin_fmax(__builtin_fmin(r, (double)kMaxBf16), -(double)kMaxBf16);
+  asm("" : "+v"(f));  // (two roundings, not one to bf16: the compiler may not join them)
+  return f;
 }
 
 // Eight channels x, rotated with their partners' y (for pairs of neighbours, y = x).  The fp32 result r is off by
 // at most 2^-24 (|x c| + 2 |y s|), r - delta and r + delta by 2^-24 (|x c| + |y s|) more; delta is 3.1 * 2^-24
-// (|x c| + |y s|), and 2^-147 for subnormal numbers.  Where r - delta and r + delta round to the same bf16 number, so does the exact value.  A wave with a
+// (|x c| + |y s|), and 2^-147 for subnormal numbers.  Where r - delta and r + delta round to the same bf16 number, so do the
+// exact value and the fp32 number next to it.  A wave with a
 // channel where they do not (1 in 10, of 512 channels each) forms its channels in 64 bits, at six times the
 // instructions.
 __device__ inline uint4 rotated(bool pairs, const uint4& x4, const uint4& y4, const Angles& g) {
@@ -405,15 +396,10 @@ __global__ __launch_bounds__(T) void k_cache_write(CacheWriteArgs a, int kv_unit
   }
 }
 
-// Eight channels as c * scale, rounded to bf16 once (a product's error in fp32 is exact by one fma).
+// Eight channels as c * scale in fp32, rounded to bf16.
 __device__ inline uint4 held_row(const float (&c)[8], float scale) {
-  float x[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x[i] = c[i] * scale;
-    x[i] = for_bf16(x[i], fmaf(c[i], scale, -x[i]));
-  }
-  return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+  return make_uint4(pack_bf16(c[0] * scale, c[1] * scale), pack_bf16(c[2] * scale, c[3] * scale),
+                    pack_bf16(c[4] * scale, c[5] * scale), pack_bf16(c[6] * scale, c[7] * scale));
 }
 
 template <int D>

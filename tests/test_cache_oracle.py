@@ -49,6 +49,7 @@ def test_to_bf16():
     x = np.clip(x, -3e38, 3e38).astype(np.float32).astype(np.float64)  # torch rounds from fp32
     assert np.array_equal(c.to_bf16(x), torch.from_numpy(x).float().to(torch.bfloat16).double().numpy())
     assert c.to_bf16(1.00390625 + 2.0 ** -40) == 1.0078125 and c.to_bf16(1.01171875 - 2.0 ** -40) == 1.0078125  # once, not by way of fp32
+    assert c.by_fp32(1.00390625 + 2.0 ** -40) == 1.0 and c.by_fp32(1.01171875 - 2.0 ** -40) == 1.015625
     assert c.to_bf16(3.4e38) == c._MAX_BF16 and c.to_bf16(-1e300) == -c._MAX_BF16
 
 

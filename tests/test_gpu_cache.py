@@ -281,14 +281,14 @@ def test_read(gpu_lib, d, page):
                 want = np.zeros((2, count[b], d))
                 m = max(0, min(s.lens_[b] - first[b], count[b]))
                 want[0, :m], want[1, :m] = kk[first[b]:first[b] + m], vv[first[b]:first[b] + m]
-                # the product in fp32, then bf16
-                want = c.to_bf16(want)
+                want = c.by_fp32(want)
                 same(f64(k[l, h, off[b]:off[b + 1]]), want[0]), (b, l, h)
                 same(f64(v[l, h, off[b]:off[b + 1]]), want[1]), (b, l, h)
     # from the start
     B.tp_cache_read(s.dims, s.cache, B.Batch(off), k, v)
     kk, vv, _ = c.held(s.pages, d, s.table[0], page, 1, 1, 263)
-    same(f64(k[1, 1, :263]), c.to_bf16(kk)) and np.array_equal(f64(v[1, 1, :263]), c.to_bf16(vv))
+    same(f64(k[1, 1, :263]), c.by_fp32(kk))
+    same(f64(v[1, 1, :263]), c.by_fp32(vv))
 
 
 # ------------------------------------------------------------------------------ attention
@@ -612,7 +612,7 @@ def test_evict_load_decode_read_evict(gpu_lib):
     B.tp_cache_read(dims, s.cache, back, k2, v2)
     for b in range(2):
         kk, vv, _ = c.held(s.pages, d, s.table[b], 32, 1, 0, m)
-        same(f64(k2[1, 0, b * m:(b + 1) * m]), c.to_bf16(kk))
+        same(f64(k2[1, 0, b * m:(b + 1) * m]), c.by_fp32(kk))
     kw["keep_budget"] = 20
     again = B.evict_fused(dims, back, qg, k2, v2, **kw)
     idx = again.kept_idx.view(L, Hkv, 40).cpu().numpy()
