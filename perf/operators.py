@@ -358,6 +358,7 @@ def _handles(st):
     n = st["offsets"][-1]
     if c["kind"] in ("load", "append", "read"):
         h["batch"] = B.Batch(st["offsets"])
+        h["first"] = [m - t for m, t in zip(_ints(c["lens"]), _new(c))] if c["kind"] == "append" else st.get("first")
         h["k"] = torch.empty((c["L"], c["Hkv"], n, c["d"]), dtype=torch.bfloat16, device="cuda")
         h["v"] = torch.empty_like(h["k"])
     if c["kind"] in ("append", "attend", "step"):
@@ -382,8 +383,7 @@ def _own_run(st):
     if c["kind"] in ("append", "step"):
         B.tp_cache_append(d, cache, h["step"], st["k"], st["v"], st["positions"], h["rope"], st["q"], h["q"])
     if c["kind"] in ("load", "append", "read"):
-        first = [m - t for m, t in zip(_ints(c["lens"]), _new(c))] if c["kind"] == "append" else st.get("first")
-        B.tp_cache_read(d, cache, h["batch"], h["k"], h["v"], first)
+        B.tp_cache_read(d, cache, h["batch"], h["k"], h["v"], h["first"])
         out = {"k": h["k"], "v": h["v"]}
         return {**out, "q": h["q"]} if c["kind"] == "append" else out
     q = h["q"] if c["kind"] == "step" else st["q"]
