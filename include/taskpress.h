@@ -404,7 +404,8 @@ typedef struct tp_cache {
 /* The new tokens of one step.  Sequence b's are rows [offsets[b], offsets[b + 1]) of the step's
  * tensors and its last ones in the cache: T_b new tokens are tokens lens[b] - T_b .. lens[b] - 1.
  * A sequence whose range is not within [0, total], decreases, or holds more than max_new tokens
- * counts as having none (its rows are left as they were), as do rows outside every range. */
+ * counts as having none (its rows are left as they were), as do rows outside every range.  Ranges that
+ * count do not overlap. */
 typedef struct tp_step {
   const int32_t* offsets; /* device [batch + 1], or NULL: row b is sequence b's one token (total >= batch) */
   int32_t total;          /* rows of the tensors along the token axis, >= 1 */

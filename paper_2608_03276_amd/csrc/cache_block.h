@@ -72,13 +72,17 @@ struct StepSeq {
 __device__ inline int32_t scalar_load(const int32_t* p) {
   return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
 }
+// Whether a sequence's range of rows counts.
+__device__ inline bool step_range(const StepArgs& s, int32_t lo, int32_t hi) {
+  return lo >= 0 && hi > lo && hi <= s.total && hi - lo <= s.max_new;
+}
 __device__ inline StepSeq step_sequence(const CacheArgs& c, const StepArgs& s, int b) {
   StepSeq q;
   q.row = b;
   q.count = 1;
   if (s.offsets != nullptr) {
     const int32_t lo = scalar_load(s.offsets + b), hi = scalar_load(s.offsets + b + 1);
-    const bool good = lo >= 0 && hi > lo && hi <= s.total && hi - lo <= s.max_new;
+    const bool good = step_range(s, lo, hi);
     q.row = good ? lo : 0;
     q.count = good ? hi - lo : 0;
   }

@@ -216,20 +216,27 @@ __device__ inline void transpose(const uint32_t (&in)[8], uint32_t (&out)[8]) {
   }
 }
 
-// Largest b with offsets[b] <= row, over batch + 1 nondecreasing entries; -1 if there is none.  The wave
-// looks at 64 entries at a time.  (Of other offsets, some b in the same range.)
-__device__ inline int sequence_of(const int32_t* offsets, int batch, int32_t row) {
+// Whether some sequence's range holds the row; the wave calls together and looks at 64 entries at a time.  In
+// nondecreasing offsets the last entry up to the row starts the only range that can hold it; where that one does
+// not (a row behind the last sequence, or offsets that fall), all ranges are looked at.
+__device__ inline bool in_a_sequence(const StepArgs& s, int batch, int32_t row) {
   const int lane = threadIdx.x & 63;
+  const auto holds = [&](int b) {
+    const int32_t lo = s.offsets[b], hi = s.offsets[b + 1];
+    return step_range(s, lo, hi) && row >= lo && row < hi;
+  };
   int base = 0, n = batch + 1;
-  for (;;) {
+  while (n > 1) {
     const int step = (n + 63) / 64;
-    const bool below = lane * step < n && offsets[base + lane * step] <= row;
-    const int found = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
-    if (found == 0) return -1;
+    const bool below = lane * step < n && s.offsets[base + lane * step] <= row;
+    const int found = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(below)), 1);
     base += (found - 1) * step;
     n = min(step, n - (found - 1) * step);
-    if (n <= 1) return base;
   }
+  if (base < batch && holds(base)) return true;
+  for (int b = 0; b < batch; b += 64)
+    if (__builtin_amdgcn_ballot_w64(b + lane < batch && holds(b + lane)) != 0) return true;
+  return false;
 }
 
 // One token's query rows.  The loads come first, then what decides whether they count.
@@ -252,10 +259,7 @@ __device__ inline void rotate_queries(const CacheWriteArgs& a, int unit) {
   if (pos < 0 || pos >= a.num_positions) return;
   Angles g = {};
   if (turn) g = load_angles(a, a.cos_sin + pos * a.rotary_dim, piece);
-  const int b = a.s.offsets == nullptr ? row : sequence_of(a.s.offsets, a.c.batch, row);
-  if (b < 0 || b >= a.c.batch) return;
-  const StepSeq q = step_sequence(a.c, a.s, b);
-  if (row < q.row || row - q.row >= q.count) return;
+  if (a.s.offsets == nullptr ? row >= a.c.batch : !in_a_sequence(a.s, a.c.batch, row)) return;
   while (h < a.Hq) {
     if (turn) x = rotated(a.pairs, x, y, g);
     // (a row's lanes are of one wave and load before they store, so q_out may be q)

@@ -292,6 +292,35 @@ def test_read(gpu_lib, d, page):
 
 
 # ------------------------------------------------------------------------------ attention
+@pytest.mark.parametrize("batch,off,total", [
+    (4, [0, 1, 2, 0, 0], 3),                                     # unused entries behind the last sequence are 0
+    (4, [0, 1, 2, -1, 0], 3),
+    (5, [4, 5, 0, 1, 3, 3], 6),                                  # sequences out of order: row 3 belongs to none
+    (200, list(range(150)) + [0] * 40 + [149, 151] + [7] * 9, 153),
+    (200, [0] * 70 + list(range(131)), 140),
+])
+def test_append_queries_of_every_sequence(gpu_lib, batch, off, total):
+    """Offsets that fall somewhere: the query rows of every range that counts are rotated, the others left alone."""
+    assert len(off) == batch + 1
+    s = Setup(19, 1, 2, 1, 64, 32, [5] * batch)
+    k, v, q = s.rows(total, 1), s.rows(total, 1), s.rows(total, 2)
+    cs, pos = table_of(9, 64), np.arange(total).astype(np.int32) % 9
+    want = np.full((total, 2, 64), -7.0)
+    for b in range(batch):
+        lo, hi = off[b], off[b + 1]
+        if lo < 0 or hi > total or hi <= lo or hi - lo > 3:
+            continue
+        for row in range(lo, hi):
+            s.write(b, 5 - hi + row, 0, 0, c.quantise_key(c.rotate(k[0, row, 0], cs[pos[row]], 64, 0)), c.quantise_value(v[0, row, 0]))
+            for h in range(2):
+                want[row, h] = c.rotate(q[0, row, h], cs[pos[row]], 64, 0)
+    q_out = torch.full((total, 2, 64), -7.0, dtype=torch.bfloat16, device="cuda")
+    B.tp_cache_append(s.dims, s.cache, B.Step(total, 3, torch.tensor(off, dtype=torch.int32, device="cuda")), bf16(k).cuda(),
+                      bf16(v).cuda(), torch.from_numpy(pos).cuda(), B.Rope(torch.from_numpy(cs).cuda(), 64), bf16(q[0]).cuda(), q_out)
+    s.check_pages()
+    same(f64(q_out), want)
+
+
 def check_attention(s, q, new, got_o, got_lse, scale, only=None, heads=None):
     """q float64 [L][total][Hq][d]; got_o, got_lse as the call wrote them; returns the worst share of the tolerance.
     only: the sequences looked at (default: all), heads: the KV heads."""
