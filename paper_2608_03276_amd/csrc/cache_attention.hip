@@ -185,7 +185,9 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
   Frag qf[kShared ? 1 : NR][KS];
   __shared__ int lds_shift[kShared ? 16 * NR : 1];  // the powers of two that the rows were multiplied by
   int shift = 0;                                    // (one tile: the lane's row's)
-  float scale[NR];  // softmax_scale * log2(e), less that power and the key scales'
+  // softmax_scale * log2(e), less that power and the key scales'
+  __shared__ float lds_scale[kShared ? W : 1][16 * NR];
+  float scale = 0.0f;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     if (kShared && r != wave) continue;  // a wave prepares one tile
@@ -223,8 +225,15 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
   if (kShared) __syncthreads();
   const auto set_scales = [&](int power) {
 #pragma unroll
-    for (int r = 0; r < NR; ++r)  // (above 0, so that an unseen token's -infinity stays one)
-      scale[r] = fmaxf(__builtin_amdgcn_ldexpf(a.scale_log2, power - (kShared ? lds_shift[r * 16 + n] : shift)), 0x1p-149f);
+    for (int r = 0; r < NR; ++r) {
+      // above 0 and finite, so that an unseen token's -infinity and a score of 0 stay that
+      const float x = __builtin_amdgcn_fmed3f(
+          __builtin_amdgcn_ldexpf(a.scale_log2, power - (kShared ? lds_shift[r * 16 + n] : shift)), 0x1p-149f, -kNoMax);
+      if (kShared)
+        lds_scale[wave][r * 16 + n] = x;
+      else
+        scale = x;
+    }
   };
   set_scales(-112);
   const auto query = [&](int r, int s) {
@@ -348,6 +357,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
     for (int r = 0; r < NR; ++r) {
       if (r > 0 && r >= tiles) break;
       float w[8], p[8], sum, top;
+      const float factor = kShared ? lds_scale[wave][r * 16 + n] : scale;
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = __uint_as_float(vs[i >> 2][i & 3]);
       if (masked) {
@@ -364,7 +374,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
         sum = top = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(fmaf(xs[i >> 2][r][i & 3], scale[r], -m[r]));
+          p[i] = __builtin_amdgcn_exp2f(fmaf(xs[i >> 2][r][i & 3], factor, -m[r]));
           sum += p[i];
           p[i] *= w[i];
           top = fmaxf(top, p[i]);
@@ -375,7 +385,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
         float next = kNoMax;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          next = fmaxf(next, fmaf(xs[i >> 2][r][i & 3], scale[r], __builtin_amdgcn_logf(fmaxf(w[i], kLeastScale)) - kSet));
+          next = fmaxf(next, fmaf(xs[i >> 2][r][i & 3], factor, __builtin_amdgcn_logf(fmaxf(w[i], kLeastScale)) - kSet));
         }
         next = fmaxf(row_max(next), m[r]);
         const float f = __builtin_amdgcn_exp2f(m[r] - next);

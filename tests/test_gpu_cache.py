@@ -516,6 +516,21 @@ def test_attention_scales_far_apart(gpu_lib):
         check_attention(s, q, [2, 1], f64(out), f64(lse), scale)
 
 
+def test_attention_of_large_rows_at_right_angles(gpu_lib):
+    """Queries and keys whose largest channels' product is beyond fp32, in different channels: every score is 0."""
+    s = Setup(41, 1, 4, 1, 128, 64, [100])
+    blocks = s.pages.reshape(-1, c.block_bytes(128))
+    blocks[:, :16 * 128].reshape(-1, 32, 16, 4)[:, :, 0::4] = 0x88  # channels 0..31 of the keys: zeros
+    ks = c.bf16_bits(np.full((len(blocks), 128), 2.0 ** 120)).view(np.uint8)
+    blocks[:, 32 * 128:34 * 128] = ks.reshape(len(blocks), -1)
+    s.upload()
+    q = s.rows(2, 4) * 2.0 ** 120
+    q[..., 32:] = 0
+    q = c.to_bf16(q)
+    out, lse = attend(s, q, [2], 1.0)
+    check_attention(s, q, [2], f64(out), f64(lse), 1.0)
+
+
 def test_attention_strides(gpu_lib):
     """Queries inside a fused projection's rows, head-major queries and outputs, and an output between guards."""
     s = Setup(34, 1, 8, 2, 64, 32, [90, 41])
