@@ -485,7 +485,8 @@ tp_status tp_cache_workspace_size(const tp_dims* dims, const tp_cache* cache, co
  *   lse[l][r][row] = ln sum_p exp(x_p)
  * for every query head r of KV head r / (Hq / Hkv).  A row that attends to nothing (an empty
  * sequence, t < T_b - lens[b], pages missing throughout) gets o = 0 and lse = -infinity.
- * q, o rows of Hq heads; o is rounded to bf16 once; lse fp32 [L][Hq][total], 4-byte aligned, or NULL.
+ * q, o rows of Hq heads; o may be q (the same data and strides).  o is rounded to bf16 once; lse fp32
+ * [L][Hq][total], 4-byte aligned, or NULL.
  * max_len: at least every lens[b] (host; in [1, max_pages * page_tokens]); a longer sequence counts
  * as empty.  softmax_scale > 0, finite.  Scores beyond fp32's range give what fp32 gives.
  * workspace: device, >= tp_cache_workspace_size() bytes, 256-byte aligned (NULL if that is 0).

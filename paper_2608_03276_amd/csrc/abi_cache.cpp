@@ -98,6 +98,13 @@ tp_status check_rows(const tp_dims* d, int32_t heads, int32_t total, const tp_ro
   return TP_OK;
 }
 
+// Rows of q heads written where they are read: every row in its own place.
+bool in_place_or_apart(const tp_dims* d, int32_t total, const tp_rows* from, const tp_rows* to) {
+  return from->data != to->data || ((d->num_layers == 1 || from->layer_stride == to->layer_stride) &&
+                                    (total == 1 || from->token_stride == to->token_stride) &&
+                                    (d->num_q_heads == 1 || from->head_stride == to->head_stride));
+}
+
 // A launch's x dimension holds fewer than 2^32 work-items.
 bool fits_grid(double workgroups, double threads = 256.0) { return workgroups * threads < 0x1p32; }
 
@@ -206,10 +213,7 @@ tp_status tp_cache_append(const tp_dims* dims, const tp_cache* cache, const tp_s
     s = check_rows(dims, dims->num_q_heads, step->total, q, false, "q", a.q);
     if (s == TP_OK) s = check_rows(dims, dims->num_q_heads, step->total, q_out, true, "q_out", a.q_out);
     if (s != TP_OK) return s;
-    if (q->data == q_out->data &&
-        ((dims->num_layers > 1 && q->layer_stride != q_out->layer_stride) ||
-         (step->total > 1 && q->token_stride != q_out->token_stride) ||
-         (dims->num_q_heads > 1 && q->head_stride != q_out->head_stride)))
+    if (!in_place_or_apart(dims, step->total, q, q_out))
       return fail(TP_ERR_SHAPE, "q_out on q's memory must have q's strides");
   }
   a.Hq = dims->num_q_heads;
@@ -289,6 +293,7 @@ tp_status tp_cache_attention(const tp_dims* dims, const tp_cache* cache, const t
     return fail(TP_ERR_WORKSPACE, "workspace needs %zu bytes (got %zu%s)", plan.total, ws_bytes,
                 workspace ? "" : ", NULL");
   if (((uintptr_t)workspace & 255u) != 0) return fail(TP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (!in_place_or_apart(dims, step->total, q, o)) return fail(TP_ERR_SHAPE, "o on q's memory must have q's strides");
   a.lse = lse;
   a.stat = (float2*)((char*)workspace + plan.stat_off);
   a.part = (float*)((char*)workspace + plan.o_off);

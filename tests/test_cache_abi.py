@@ -141,6 +141,7 @@ def test_attention_refusals():
         assert _attend(o=r) == want
     for r in OVERLAPS:
         assert _attend(o=r) == B.TP_ERR_SHAPE
+    assert _attend(q=out_rows(), o=out_rows(layer=8 * 1024)) == B.TP_ERR_SHAPE  # q's memory at other strides
     for scale in (0.0, -1.0, float("inf"), float("nan"), 3e38):
         assert _attend(scale=scale) == B.TP_ERR_PARAM
     assert _attend(most=0) == _attend(most=321) == B.TP_ERR_SHAPE

@@ -557,6 +557,18 @@ def test_attention_strides(gpu_lib):
     assert torch.equal(out, same[0])
 
 
+@pytest.mark.parametrize("lens,new", [([90, 41], [3, 2]), ([9000, 70], [17, 1]), ([300], [100]), ([2000, 0], [1, 1])])
+def test_attention_in_place(gpu_lib, lens, new):
+    """Outputs on the queries' memory, with one to four tiles of rows, whole and in chunks."""
+    s = Setup(42, 1, 8, 2, 128, 64, lens)
+    q = s.rows(sum(new), 8)
+    want, wl = attend(s, q, new, 0.1, max_len=max(lens))
+    rows, lse = bf16(q).cuda(), torch.empty_like(wl)
+    step = B.Step(sum(new), max(new), torch.from_numpy(offsets_of(new)).cuda())
+    B.tp_cache_attention(s.dims, s.cache, step, rows, 0.1, max(lens), rows, lse)
+    assert torch.equal(rows, want) and torch.equal(lse, wl)
+
+
 def test_one_token_without_offsets_and_padded_batch(gpu_lib):
     """offsets = NULL: row b is sequence b's token; padded sequences have length 0, rows behind the batch stay."""
     s = Setup(35, 1, 8, 2, 128, 64, [100, 0, 33, 0], cols=2)
