@@ -446,7 +446,7 @@ size_t tp_cache_page_bytes(const tp_dims* dims, int32_t page_tokens);
  * kept_offsets: host [batch + 1] from 0, nondecreasing, k_b <= max_pages * page_tokens (TP_ERR_SHAPE);
  * k bf16 [L][Hkv][K_tot][d], v_q bytes [L][Hkv][K_tot][d / 2], scales fp32 [L][Hkv][K_tot], contiguous,
  * 16-byte aligned.  cache->batch <= TP_MAX_BATCH.  bits in [2, 4], the bits v_q was quantised with.
- * The keys are finite.  lens is neither read nor set.
+ * The keys are finite.  lens is neither read nor set.  The pages written are listed once.
  * Errors: TP_ERR_NULL, TP_ERR_SHAPE, TP_ERR_PARAM, TP_ERR_UNSUPPORTED, TP_ERR_HIP.
  */
 tp_status tp_cache_load(const tp_dims* dims, const tp_cache* cache, const int64_t* kept_offsets, const void* k,
