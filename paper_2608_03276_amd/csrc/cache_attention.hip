@@ -19,8 +19,8 @@
 //
 // Measured at d = 128: one row tile is bound by HBM (64 sequences of 6K to 32K tokens, 64 query heads: 1.16 GB in
 // 222 us, 5.2 TB/s; two of 262144 and 131073: 440 MB in 76 us), four by the vector ALU (chunks of 1024 and 300
-// tokens against 17333 and 4096, 32 query heads: 302 GFLOP in 336 us).  Of 271 vector instructions a block and
-// tile, 176 turn codes into operands.
+// tokens against 17333 and 4096, 32 query heads: 302 GFLOP in 329 us).  Of 270 vector instructions a block with
+// one tile, 461 with four, 176 turn codes into operands.
 //
 // The running reference m of a row bounds the weights that are rounded, p * scale of the value, not p alone:
 // p = exp2(x - m) and the sum of the p's are fp32, in which the reference may be anywhere.
@@ -312,10 +312,14 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
   for (int j = j0; j < j1; j += W) {
     const bool missing = page_of(j) < 0;
     const bool masked = missing || (j + 1) * kCacheBlock > all_seen;
-    if (masked) {  // scales of slots that no row sees may be anything
+    if (masked) {  // scales of slots that no row sees may be anything, of those that one does not see must be finite
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
         if (missing || j * kCacheBlock + u * 16 + n >= rg.keys) ks[u] = (u32x2){0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          vs[u][i] = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(vs[u][i]), 0.0f, -kNoMax));
+      }
     }
     // Key scales to fp16: bf16 bits, with the exponent brought into range and the mantissa moved by 3 bits.
     const u16x2 top2 = max_pair(max_pair(pair(ks[0].x), pair(ks[1].x)), max_pair(pair(ks[0].y), pair(ks[1].y)));
@@ -370,19 +374,15 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
         const int seen = missing || row >= rg.rows ? 0 : rg.before + a.R.div(row) + 1;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (j * kCacheBlock + (i >> 2) * 16 + g * 4 + (i & 3) >= seen) {
-            xs[i >> 2][r][i & 3] = -INFINITY;
-            w[i] = 0.0f;  // (the slot may hold anything)
-          }
+          if (j * kCacheBlock + (i >> 2) * 16 + g * 4 + (i & 3) >= seen) xs[i >> 2][r][i & 3] = -INFINITY;
       }
       const auto weigh = [&] {
-        sum = top = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           p[i] = __builtin_amdgcn_exp2f(fmaf(xs[i >> 2][r][i & 3], factor, -m[r]));
-          sum += p[i];
+          sum = i == 0 ? p[i] : sum + p[i];
           p[i] *= w[i];
-          top = fmaxf(top, p[i]);
+          top = i == 0 ? p[i] : fmaxf(top, p[i]);
         }
       };
       weigh();
