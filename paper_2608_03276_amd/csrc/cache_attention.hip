@@ -528,10 +528,15 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache_merge(CacheAttnArgs a) 
 }  // namespace
 
 // Chunks: merging costs a launch (4 us) and, for each row and chunk, 4 d + 8 bytes written and read.
-//  - Rows of one or two tiles (decoding, drafts): chunks of 4096 tokens where the (sequence, head) pairs alone
-//    occupy every CU (32 sequences of 8 heads and 2049 to 2548 tokens: 27.2 us whole, 29.9 in chunks of 640);
-//    otherwise about 1024 workgroups, in chunks of 512 at least (one sequence of 13215, 8 heads: 11.1 us at 512, 13.5
-//    at 1024, 25.9 at 4096; two of 262144 and 131073: 78.0 us at 4096, 92.1 at 1024, 94.1 at 8192).
+//  - Rows of one or two tiles (decoding, drafts): chunks of 4096 tokens where the (sequence, head) pairs occupy
+//    every CU (32 sequences of 8 heads and 2049 to 2548 tokens: 27.2 us whole, 29.9 in chunks of 640); fewer pairs
+//    get about 1024 workgroups, in chunks of 512 at least (one sequence of 13215, 8 heads: 11.1 us at 512, 13.5
+//    at 1024, 25.9 at 4096; two of 262144 and 131073: 78.0 us at 4096, 92.1 at 1024, 94.1 at 8192), unless
+//    what the idle CUs would take, n (1 - pairs / CUs), is less than the split costs: about 960 tokens of a CU with
+//    one tile, 640 with two (8 heads; split and whole: one sequence of 520 tokens 8.5 and 7.3 us, of 1024 9.0 and
+//    9.2; 8 of 800 9.4 and 8.6, of 1400 10.0 and 11.0; 17 of 2048 15.9 and 14.6, of 4096 22.8 and 23.4; 25 of 2600
+//    21.9 and 17.6, and with lengths down to a tenth of that 18.8 and 17.3; two tiles: 8 of 1024 12.8 and 14.2, 20
+//    of 1024 18.2 and 15.1).
 //    Whole sequences of at most two workgroups a CU take eight waves (those 32 sequences: 26.2 us with four, 23.4
 //    with eight, the append before it 5.8 of them; 64 of 6K to 32K tokens in chunks: 235 and 249).
 //  - Four tiles (prompts): whole sequences from 1024 workgroups on, fewer are brought to that number.
@@ -546,7 +551,8 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
   const int64_t heads = (int64_t)L * Hkv * batch, units = heads * p.row_groups;
   const int64_t n = max_len, finest = (n + kLeast - 1) / kLeast, whole = (n + kWhole - 1) / kWhole;
   const int64_t fill = std::min(finest, (kWorkgroups + units - 1) / units);
-  int64_t chunks = p.tiles == 4 ? fill : units >= kCus ? whole : std::max(whole, fill);
+  const bool few_idle = n * (kCus - units) <= (p.tiles == 1 ? 960 : 640) * kCus;
+  int64_t chunks = p.tiles == 4 ? fill : few_idle ? whole : std::max(whole, fill);
   p.chunk = (int32_t)(((n + chunks - 1) / chunks + kUnit - 1) / kUnit * kUnit);
   p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
   // Partial rows: up to 32 a pair in chunks of kWhole, up to 64 (kWorkgroups + units) in the fill.  The bound
