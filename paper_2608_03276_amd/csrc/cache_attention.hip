@@ -539,7 +539,11 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache_merge(CacheAttnArgs a) 
 //    of 1024 18.2 and 15.1).
 //    Whole sequences of at most two workgroups a CU take eight waves (those 32 sequences: 26.2 us with four, 23.4
 //    with eight, the append before it 5.8 of them; 64 of 6K to 32K tokens in chunks: 235 and 249).
-//  - Four tiles (prompts): whole sequences from 1024 workgroups on, fewer are brought to that number.
+//  - Four tiles (prompts): the least cost of the busiest CU, in blocks of the cache: those of its workgroups (0.3 us
+//    each; with one workgroup a CU half as much again), and, where there are chunks, 16 a workgroup for its partial
+//    rows and 6 for the merge.  Measured with 32 query, 8 KV heads: 256 new tokens against 4096 in 4 chunks 36 us, in
+//    2 40, in 8 50; 512 against 1024 whole 22, in 2 29; 1024 against 4096 whole 83, in 2 100; 64 against 1024 in 2 18,
+//    whole 21.
 CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
                      int32_t max_len) {
   constexpr int64_t kUnit = 128;  // tokens: a block for each of four waves
@@ -550,9 +554,23 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
   p.row_groups = (int32_t)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
   const int64_t heads = (int64_t)L * Hkv * batch, units = heads * p.row_groups;
   const int64_t n = max_len, finest = (n + kLeast - 1) / kLeast, whole = (n + kWhole - 1) / kWhole;
-  const int64_t fill = std::min(finest, (kWorkgroups + units - 1) / units);
-  const bool few_idle = n * (kCus - units) <= (p.tiles == 1 ? 960 : 640) * kCus;
-  int64_t chunks = p.tiles == 4 ? fill : few_idle ? whole : std::max(whole, fill);
+  int64_t chunks;
+  if (p.tiles == 4) {
+    int64_t least = 0;
+    chunks = 0;
+    for (int64_t w = 0; w <= 8; ++w) {  // whole, and the most chunks of w workgroups a CU
+      const int64_t c = w == 0 ? 1 : std::min(finest, w * kCus / units);
+      if (c <= chunks) continue;
+      const int64_t each = (units * c + kCus - 1) / kCus, blocks = each * ((n + c * kCacheBlock - 1) / (c * kCacheBlock));
+      const int64_t cost = (each == 1 ? blocks * 3 / 2 : blocks) + (c == 1 ? 0 : 6 + 16 * each);
+      if (chunks != 0 && cost >= least) continue;
+      chunks = c;
+      least = cost;
+    }
+  } else {
+    const bool few_idle = n * (kCus - units) <= (p.tiles == 1 ? 960 : 640) * kCus;
+    chunks = few_idle ? whole : std::max(whole, std::min(finest, (kWorkgroups + units - 1) / units));
+  }
   p.chunk = (int32_t)(((n + chunks - 1) / chunks + kUnit - 1) / kUnit * kUnit);
   p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
   // Partial rows: up to 32 a pair in chunks of kWhole, up to 64 (kWorkgroups + units) in the fill.  The bound
