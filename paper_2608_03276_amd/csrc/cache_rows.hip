@@ -7,8 +7,8 @@
 // one workgroup of the launch, so nothing races.  Everything that a workgroup loads hangs on the sequence's
 // offsets and length alone, but for the angles (on the positions) and the old values (on the page).
 //
-// Bound by HBM (d = 128): 13107 kept tokens of 32 layers and 8 heads into pages in 333 us (5.6 TB/s) and back in 409
-// (4.6, four fifths of it writes); 12290 new tokens of 64 query and 8 KV heads in 105 us (4.5 TB/s).  A decoding
+// Bound by HBM (d = 128): 13107 kept tokens of 32 layers and 8 heads into pages in 300 us (6.2 TB/s) and back in 428
+// (4.4, four fifths of it writes); 12290 new tokens of 64 query and 8 KV heads in 105 us (4.5 TB/s).  A decoding
 // step's append is latency: 64 sequences in 5.9 us.
 #include "cache_block.h"
 #include "quant_row.h"
@@ -410,7 +410,25 @@ __device__ inline uint4 held_row(const float (&c)[8], float scale) {
                     pack_bf16(c[4] * scale, c[5] * scale), pack_bf16(c[6] * scale, c[7] * scale));
 }
 
-template <int D>
+// 16 bytes that pass once: ONCE leaves them out of the caches.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <bool ONCE>
+__device__ inline uint4 load16(const uint4* p) {
+  if (!ONCE) return *p;
+  const u32x4 x = __builtin_nontemporal_load((const u32x4*)p);
+  return make_uint4(x.x, x.y, x.z, x.w);
+}
+template <bool ONCE>
+__device__ inline void store16(uint4* p, const uint4& x) {
+  if (ONCE)
+    __builtin_nontemporal_store((u32x4){x.x, x.y, x.z, x.w}, (u32x4*)p);
+  else
+    *p = x;
+}
+
+// ONCE: the rows are more than the chip's caches hold, so no later kernel finds them there (8 layers and heads, 27000
+// tokens: 254 us, 240 with it).
+template <int D, bool ONCE>
 __global__ __launch_bounds__(kRowsThreads) void k_cache_read(CacheReadArgs a) {
   using B = CacheBlock<D>;
   constexpr int LPT = D / 8, kPasses = kCacheBlock * LPT / kRowsThreads;
@@ -427,7 +445,7 @@ __global__ __launch_bounds__(kRowsThreads) void k_cache_read(CacheReadArgs a) {
   uint32_t kw[kPasses], ks[kPasses];
   float vs[kPasses];
   if (blk != nullptr) {
-    if (threadIdx.x < D) words[threadIdx.x] = *((const uint4*)(blk + B::kValues) + threadIdx.x);
+    if (threadIdx.x < D) words[threadIdx.x] = load16<ONCE>((const uint4*)(blk + B::kValues) + threadIdx.x);
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
       const int slot = p * (kRowsThreads / LPT) + (int)threadIdx.x / LPT;
@@ -458,8 +476,8 @@ __global__ __launch_bounds__(kRowsThreads) void k_cache_read(CacheReadArgs a) {
       v = held_row(c, vs[p]);
     }
     const int64_t to = (int64_t)lh * a.off[a.c.batch] + a.off[b] + (t - first);
-    *((uint4*)(a.k + to * D) + piece) = k;
-    *((uint4*)(a.v + to * D) + piece) = v;
+    store16<ONCE>((uint4*)(a.k + to * D) + piece, k);
+    store16<ONCE>((uint4*)(a.v + to * D) + piece, v);
   }
 }
 
@@ -501,10 +519,15 @@ hipError_t launch_cache_load(CacheWriteArgs& a, int head_dim, hipStream_t stream
 hipError_t launch_cache_read(CacheReadArgs& a, int head_dim, hipStream_t stream) {
   const dim3 grid((unsigned)(a.c.L * a.c.Hkv * a.blocks), (unsigned)a.c.batch);
   set_heads(a);
-  if (head_dim == 128)
-    hipLaunchKernelGGL(k_cache_read<128>, grid, dim3(kRowsThreads), 0, stream, a);
+  const bool once = (double)a.c.L * a.c.Hkv * (double)a.off[a.c.batch] * head_dim * 4.0 > (double)(256 << 20);
+  if (head_dim == 128 && once)
+    hipLaunchKernelGGL((k_cache_read<128, true>), grid, dim3(kRowsThreads), 0, stream, a);
+  else if (head_dim == 128)
+    hipLaunchKernelGGL((k_cache_read<128, false>), grid, dim3(kRowsThreads), 0, stream, a);
+  else if (once)
+    hipLaunchKernelGGL((k_cache_read<64, true>), grid, dim3(kRowsThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL(k_cache_read<64>, grid, dim3(kRowsThreads), 0, stream, a);
+    hipLaunchKernelGGL((k_cache_read<64, false>), grid, dim3(kRowsThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -291,6 +291,22 @@ def test_read(gpu_lib, d, page):
     same(f64(v[1, 1, :263]), c.by_fp32(vv))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_read_more_than_the_caches_hold(gpu_lib, d):
+    """Outputs above 256 MB (streaming stores): the same rows, zeros behind the sequences, rows outside the ranges kept."""
+    s = Setup(23, 1, 8, 8, d, 64, [300, 97])
+    few = torch.empty((8, 397, d), dtype=torch.bfloat16, device="cuda")
+    fewv = torch.empty_like(few)
+    B.tp_cache_read(s.dims, s.cache, B.Batch([0, 297, 397]), few, fewv, [3, 0])
+    n = (1 << 28) // (8 * d * 4) + 333
+    k = torch.full((1, 8, n, d), -7.0, dtype=torch.bfloat16, device="cuda")
+    v = torch.full_like(k, -7.0)
+    B.tp_cache_read(s.dims, s.cache, B.Batch([0, 297, n]), k, v, [3, 0])
+    for got, want in ((k, few), (v, fewv)):
+        assert torch.equal(got[0, :, :394], want[:, :394])
+        assert not bool(got[0, :, 394:].any())
+
+
 # ------------------------------------------------------------------------------ attention
 @pytest.mark.parametrize("batch,off,total", [
     (4, [0, 1, 2, 0, 0], 3),                                     # unused entries behind the last sequence are 0
