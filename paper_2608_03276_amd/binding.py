@@ -6,6 +6,7 @@ machine without the built library raises ImportError (there is no fallback).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -196,6 +197,22 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _made_on(stream, device):
+    """Tensors made within come from the allocator's pool of the call's stream, which writes them: another stream's
+    pool may hand out memory that what is queued there still uses, and takes it back before the call's work is done."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
+def _workspace(nbytes: int, device, stream):
+    with _made_on(stream, device):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _need(t, numel, name, device=True):
     if t is None:
         return
@@ -268,8 +285,7 @@ def tp_guide_attention(d: TpDims, batch: Batch, q_guide, k, v, softmax_scale: fl
     _need(o_guide, L * Hq * batch.g_tot * D * 4, "o_guide")
     _need(guide_lse, L * Hq * batch.g_tot * 4, "guide_lse")
     if workspace is None:
-        workspace = torch.empty(tp_workspace_size(TP_FN_GUIDE_ATTENTION, d, batch), dtype=torch.uint8,
-                                device=q_guide.device)
+        workspace = _workspace(tp_workspace_size(TP_FN_GUIDE_ATTENTION, d, batch), q_guide.device, stream)
     _check(load().tp_guide_attention(ctypes.byref(d), ctypes.byref(batch.c), _ptr(q_guide), _ptr(k), _ptr(v),
                                      _ptr(k_guide), _ptr(v_guide), float(softmax_scale), _ptr(o_guide),
                                      _ptr(guide_lse), _ptr(workspace), _nbytes(workspace), _stream(stream)))
@@ -291,8 +307,7 @@ def tp_guide_attention_quantize(d: TpDims, batch: Batch, q_guide, k, v, softmax_
     _need(scales, L * Hkv * batch.n_tot * 4, "scales")
     _need(v_q, L * Hkv * batch.n_tot * row_bytes(qfmt, bits, D), "v_q")
     if workspace is None:
-        workspace = torch.empty(tp_workspace_size(TP_FN_GUIDE_ATTENTION, d, batch), dtype=torch.uint8,
-                                device=q_guide.device)
+        workspace = _workspace(tp_workspace_size(TP_FN_GUIDE_ATTENTION, d, batch), q_guide.device, stream)
     _check(load().tp_guide_attention_quantize(ctypes.byref(d), ctypes.byref(batch.c), _ptr(q_guide), _ptr(k),
                                               _ptr(v), _ptr(k_guide), _ptr(v_guide), float(softmax_scale),
                                               int(qfmt), int(bits), _ptr(o_guide), _ptr(guide_lse), _ptr(scales),
@@ -329,8 +344,7 @@ def tp_combine_select_topk(d: TpDims, batch: Batch, s_key, scales, rule: int, ke
     _need(s_out, L * Hkv * batch.n_tot * 4, "s_out")
     ko = _i64_array(kept_offsets)
     if workspace is None:  # the caller passed none: one of the size the library asks for
-        workspace = torch.empty(tp_workspace_size(TP_FN_COMBINE_SELECT_TOPK, d, batch), dtype=torch.uint8,
-                                device=s_key.device)
+        workspace = _workspace(tp_workspace_size(TP_FN_COMBINE_SELECT_TOPK, d, batch), s_key.device, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check(load().tp_combine_select_topk(ctypes.byref(d), ctypes.byref(batch.c), _ptr(s_key), _ptr(scales),
                                          int(rule), float(keep_ratio), int(keep_budget), ko, _ptr(kept_idx),
@@ -393,10 +407,12 @@ class EvictBuffers:
 def evict(d: TpDims, batch: Batch, q_guide, k, v, *, softmax_scale: float, pool_k: int, qfmt: int, bits: int,
           rule: int = TP_COMBINE_MUL, keep_ratio: float = 0.0, keep_budget: int = 0, bufs: EvictBuffers = None,
           stream=None, k_guide=None) -> EvictBuffers:
-    """Run the four steps on one stream; returns the buffers (kept_idx, k_c, v_q_c, scales_c, ...)."""
+    """Run the four steps on one stream; returns the buffers (kept_idx, k_c, v_q_c, scales_c, ...), made on that stream
+    unless given."""
     ko = kept_offsets_for(batch, keep_ratio, keep_budget)
     if bufs is None:
-        bufs = EvictBuffers(d, batch, qfmt, bits, ko, device=k.device)
+        with _made_on(stream, k.device):
+            bufs = EvictBuffers(d, batch, qfmt, bits, ko, device=k.device)
     tp_guide_scores(d, batch, q_guide, k, softmax_scale, pool_k, bufs.s_key, bufs.ws_evict, stream, k_guide)
     tp_quantize_v_scales(d, batch, v, qfmt, bits, bufs.scales, bufs.v_q, stream)
     tp_combine_select_topk(d, batch, bufs.s_key, bufs.scales, rule, keep_ratio, keep_budget, ko, bufs.kept_idx,
@@ -462,12 +478,14 @@ def evict_fused(d: TpDims, batch: Batch, q_guide, k, v, *, softmax_scale: float,
                 bits: int, rule: int = TP_COMBINE_MUL, keep_ratio: float = 0.0, keep_budget: int = 0,
                 bufs: EvictBuffers = None, events=None, stream=None, k_guide=None, guide_lse=None,
                 full_codes: bool = True) -> EvictBuffers:
-    """The whole path through tp_evict; returns the buffers (kept_idx, k_c, v_q_c, scales_c, ...).
+    """The whole path through tp_evict; returns the buffers (kept_idx, k_c, v_q_c, scales_c, ...), made on the
+    call's stream unless given.
     full_codes=False: no code tensor for every token (bufs.v_q untouched); the compaction
     quantises the kept rows."""
     ko = kept_offsets_for(batch, keep_ratio, keep_budget)
     if bufs is None:
-        bufs = EvictBuffers(d, batch, qfmt, bits, ko, device=k.device)
+        with _made_on(stream, k.device):
+            bufs = EvictBuffers(d, batch, qfmt, bits, ko, device=k.device)
     tp_evict(d, batch, q_guide, k, v, softmax_scale, pool_k, qfmt, bits, rule, keep_ratio, keep_budget, ko,
              bufs.s_key, bufs.scales, bufs.v_q if full_codes else None, bufs.s_comb, bufs.kept_idx, bufs.k_c,
              bufs.v_q_c, bufs.scales_c, bufs.ws_evict, events, stream, k_guide, guide_lse)
@@ -631,9 +649,7 @@ def tp_cache_attention(d: TpDims, cache: Cache, step: Step, q, softmax_scale: fl
     if lse is not None:
         _need(lse, L * Hq * n * 4, "lse")
     if workspace is None:
-        workspace = torch.empty(tp_cache_workspace_size(d, cache, step, max_len), dtype=torch.uint8, device=cache.device)
-        if stream is not None:  # allocated on the current stream: kept until the work on the other one is done
-            workspace.record_stream(torch.cuda.ExternalStream(s, device=cache.device))
+        workspace = _workspace(tp_cache_workspace_size(d, cache, step, max_len), cache.device, stream)
     _on_device(cache, load().tp_cache_attention, byref(d), cache.ref, step.ref, byref(_rows(q, L, n, Hq, D, "q")),
                softmax_scale, max_len, byref(_rows(o, L, n, Hq, D, "o")), _ptr(lse), workspace.data_ptr(),
                _nbytes(workspace), s)
