@@ -139,11 +139,12 @@ __device__ inline int64_t partial_row(const CacheAttnArgs& a, int chunk, int b, 
   return (((int64_t)chunk * a.c.batch + b) * (int)a.heads.d + lh) * ((int64_t)a.R.d * a.s.max_new) + row;
 }
 
-// CH channels of a row from c0: the sum of weighted values over the sum of weights (st.y), and the log-sum-exp.
+// CH channels of a row from c0: the sum of weighted values over the sum of weights (st.y), and the log-sum-exp.  The sum
+// is 0 where no key was seen, and NaN (with every channel's) where a score was +infinity or NaN.
 template <int CH>
 __device__ inline void store_output(const CacheAttnArgs& a, int layer, int64_t token, int hq, int c0, const float (&o)[CH],
                                     const float2& st) {
-  const float inv = st.y > 0.0f ? 1.0f / st.y : 0.0f;
+  const float inv = st.y == 0.0f ? 0.0f : 1.0f / st.y;
   uint16_t* to = a.o.data + layer * a.o.layer + token * a.o.token + hq * a.o.head + c0;
   typedef __bf16 bf16s __attribute__((ext_vector_type(CH)));
   bf16s v;
@@ -152,7 +153,7 @@ __device__ inline void store_output(const CacheAttnArgs& a, int layer, int64_t t
   *(bf16s*)to = v;
   if (a.lse != nullptr && c0 == 0)
     a.lse[((int64_t)layer * a.Hq + hq) * a.s.total + token] =
-        st.y > 0.0f ? (st.x + __builtin_amdgcn_logf(st.y)) * kLn2 : -INFINITY;
+        st.y == 0.0f ? -INFINITY : (st.x + __builtin_amdgcn_logf(st.y)) * kLn2;
 }
 
 // NR tiles of 16 rows, W waves.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave it out).

@@ -50,3 +50,59 @@ def test_scratch_of_the_calls_stream(gpu_lib, monkeypatch, how):
     assert made == [on.cuda_stream]
     assert torch.equal(out, want[0]) and torch.equal(l, lse[0])
     assert bool((kept == 3).all())
+
+
+# ------------------------------------------------------------------------------ scores that fp32 does not hold
+@pytest.mark.parametrize("n", [90, 700, 9000])
+@pytest.mark.parametrize("T_", [1, 6, 12, 20])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_scores_beyond_fp32(gpu_lib, d, T_, n):
+    """A row with a score of +infinity or NaN has no softmax: o and lse are NaN, not those of a row that sees nothing.
+    A score of -infinity is a key that is not seen.  The rows beside it keep their results.
+
+    Ordinary rows: a group's |q| sums to 26 * 2^-62 (at most 40 here) under scales of 2^60, so delta of test_gpu_cache.py is
+    4 * 40/4 * 72 * 7 * 2^-24 = 2^-9.7 for these; 2^-10 of the log-sum-exp holds with 26, 2^-10.9 + 2 delta + 2^-14 is 2^-8.5."""
+    s = T.Setup(72, 1, 4, 2, d, 64, [n])
+    blocks = s.pages.reshape(-1, 2, s.page // 32, c.block_bytes(d))  # [page][head][block]
+    blocks[..., :16 * d].reshape(*blocks.shape[:3], 32, 4, d // 32, 4)[..., 0, :] = 0xFF  # channels 0..31: codes 7
+    ks = c.bf16_bits(np.full((*blocks.shape[:3], 32, d // 32), 2.0 ** 60))
+    ks[:, 1, :, ::3] = 0  # head 1: every third key is zero
+    blocks[..., 32 * d:34 * d] = ks.reshape(*blocks.shape[:3], -1).view(np.uint8)
+    s.upload()
+    kinds = ["ordinary", "up", "down", "nan", "inf", "both"]
+    q = s.rows(T_, 4) * 2.0 ** -62
+    for t in range(T_):
+        kind = kinds[(t + 1) % 6] if T_ > 1 else "up"
+        if kind in ("up", "down", "both"):
+            q[0, t] = 0.0
+            q[0, t, :, :32] = {"up": 1, "down": -1, "both": 1}[kind] * 2.0 ** 70
+            if kind == "both":  # the two heads of a KV head: one row up, one ordinary
+                q[0, t, ::2] = s.rows(1, 4)[0, 0, ::2] * 2.0 ** -62
+    q = c.to_bf16(q)
+    finite = q.copy()
+    for t in range(T_):
+        kind = kinds[(t + 1) % 6] if T_ > 1 else "up"
+        if kind in ("nan", "inf"):
+            q[0, t, :, 5] = np.nan if kind == "nan" else np.inf
+    out, lse = T.attend(s, q, [T_], 1.0)
+    out, lse = T.f64(out)[0], T.f64(lse)[0]
+    held = [c.held(s.pages, d, s.table[0], s.page, 0, h, n) for h in range(2)]
+    for t in range(T_):
+        kind = kinds[(t + 1) % 6] if T_ > 1 else "up"
+        for h in range(4):
+            tag, got, l = (kind, t, h), out[t, h], lse[h, t]
+            if kind in ("up", "nan", "inf") or (kind == "both" and h % 2 == 1):
+                assert np.isnan(l) and np.isnan(got).all(), (tag, l, got[:4])
+            elif kind == "down" and h < 2:  # every score is -infinity
+                assert l == -math.inf and not got.any(), (tag, l)
+            elif kind == "down":            # the zero keys' mean
+                v = held[1][1][:n - T_ + t + 1:1]
+                v = v[np.abs(held[1][0][:len(v)]).max(1) == 0]
+                assert abs(l - math.log(len(v))) <= 2.0 ** -13, (tag, l)
+                tol = np.abs(v).mean(0) * (2.0 ** -10.9 + 2.0 ** -14) + 2.0 ** -8 * np.abs(v.mean(0)) + n * 2.0 ** -30 * np.abs(v).max()
+                assert np.all(np.abs(got - v.mean(0)) <= tol), tag
+            else:
+                k, v, _ = held[h // 2]
+                ref, want, mag = c.attend(finite[0, t, h], k, v, np.arange(n) <= n - T_ + t, 1.0)
+                assert abs(l - want) <= 2.0 ** -10, (tag, l, want)
+                assert np.all(np.abs(got - ref) <= mag * 2.0 ** -8.5 + 2.0 ** -8 * np.abs(ref) + n * 2.0 ** -30 * np.abs(v).max()), tag
