@@ -493,8 +493,9 @@ tp_status tp_cache_workspace_size(const tp_dims* dims, const tp_cache* cache, co
  * finite, gets o and lse NaN.
  * workspace: device, >= tp_cache_workspace_size() bytes, 256-byte aligned (NULL if that is 0).
  * Every token of a sequence that has a page holds a key and a value (was loaded or appended); what lies
- * behind the sequence's last token may be anything.  A key's scale 2^19 or more below the largest of its
- * block of 32 tokens may count as 0.
+ * behind the sequence's last token may be anything.  A channel of a query that is 2^28 or more below its row's
+ * largest is taken to within 2^-39 of that one.  A key's scale may count as 0 where it is 2^128 or more below the
+ * largest of its block of 32 tokens, or that largest times the row's largest is beyond fp32's range.
  * Maxima, sums and outputs are held in fp32; the weights times the values' scales are rounded to fp16
  * (relative to the row's largest) for the value product.
  * Errors: TP_ERR_NULL, TP_ERR_SHAPE, TP_ERR_PARAM, TP_ERR_UNSUPPORTED, TP_ERR_WORKSPACE, TP_ERR_HIP.

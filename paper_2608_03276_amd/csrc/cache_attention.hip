@@ -8,8 +8,7 @@
 //
 // Products on v_mfma_f32_16x16x32_f16, both with the cache as the A operand, so that a lane's column is one
 // query row from the scores to the output and the weights never leave their registers:
-//   scores  S^T = K Q^T: one product per group of 32 channels; its result times the group's scale is summed
-//           in fp32;
+//   scores  S^T = K Q^T: codes times their group's scale, exact in fp16, one chain of products through the groups;
 //   output  O^T += V^T P^T, with the values' scales multiplied into the weights P.
 // Codes become fp16 operands by bit operations on pairs: 0x6400 | u is 1024 + u for a 4-bit number u = c + 8,
 // and one packed fp16 operation more gives c exactly.  fp16 holds queries exactly once a row is brought near
@@ -49,11 +48,11 @@ constexpr float kSet = 8.0f, kLimit = 16384.0f;
 // with tiny or zero values cannot overflow the sum.
 constexpr float kLeastScale = 0x1p-60f;
 
-// Key scales as fp16 numbers: the largest of a block is set to exponent field 24 (2^9), and the setting is kept
-// while the largest of a block has field 20 to 27 (a code times a scale stays below 2^16).  A code times a scale
-// is exact, 3 by 8 bits in fp16's 11, down to field 1: a scale 2^19 or more below the largest of its block counts as
-// zero or one off by less than 2^-19 of that.
-constexpr int kScaleSet = 24, kScaleLow = 20 << 7, kScaleHigh = 28 << 7;
+// Key scales as fp16 numbers: a power of two for all of them sets the largest of a block to exponent field 24 (2^9),
+// and is kept while a block's scales lie in the fields 1 to 27: a code times a scale stays below 2^16 and is exact, 3 by
+// 8 bits in fp16's 11.  Where no power holds all of a block's scales (more than 2^23 between them), its scores are
+// formed in parts; the check for that costs a block no instruction more than the check of the largest alone.
+constexpr int kScaleSet = 24, kScaleLeast = 1 << 7, kScaleHigh = 28 << 7;
 
 union Frag {
   uint32_t w[4];
@@ -70,6 +69,7 @@ __device__ inline uint32_t pack_h(float lo, float hi) {
 
 __device__ inline u16x2 pair(uint32_t w) { return __builtin_bit_cast(u16x2, w); }
 __device__ inline u16x2 max_pair(u16x2 a, u16x2 b) { return __builtin_elementwise_max(a, b); }
+__device__ inline u16x2 min_pair(u16x2 a, u16x2 b) { return __builtin_elementwise_min(a, b); }
 
 // Eight codes as fp16 numbers c.  magic: 0x64006400 in a vector register (with both constants scalar, the
 // and and the or cannot be one instruction).
@@ -158,7 +158,7 @@ __device__ inline void store_output(const CacheAttnArgs& a, int layer, int64_t t
 
 // NR tiles of 16 rows, W waves.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave it out).
 template <int D, int NR, int W, bool ONCE>
-__global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache_attention(CacheAttnArgs a) {
+__global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)) void k_cache_attention(CacheAttnArgs a) {
   using B = CacheBlock<D>;
   constexpr int KS = D / 32;  // products of a score: channels in steps of 32
   constexpr int ND = D / 16;  // output tiles: channels in steps of 16
@@ -175,8 +175,10 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
   const int b = blockIdx.y;
   // 64 of the chunk's pages from page0 on, one a lane
   int page0 = (chunk * a.chunk / kCacheBlock) >> a.c.page_shift;
+  const int32_t* row_pages = a.c.table + (int64_t)b * a.c.max_pages;
   const auto load_pages = [&] {
-    return page0 + lane < a.c.max_pages ? a.c.table[(int64_t)b * a.c.max_pages + page0 + lane] : -1;
+    const uint32_t at = (uint32_t)(page0 + lane);
+    return (int)at < a.c.max_pages ? *(const int32_t*)((const char*)row_pages + 4 * at) : -1;
   };
   int pages = load_pages();
   const StepSeq q = step_sequence(a.c, a.s, b);
@@ -310,45 +312,147 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 4 : NR == 2 ? 3 : 2) void k_cache
   // the group's tiles: a decoding sequence beside a prompt's chunk has one, whose weights alone are formed
   const int tiles = (rg.rows - rg.row0 + 15) / 16;
   int bias = 0;  // bf16 bits taken off a key scale: it becomes an fp16 number times 2^(bias / 128 - 112)
+  // A key scale's bits, opaque, so that nothing formed from it is kept in registers over the loop.
+  const auto scale_of = [&](int u, int s) {
+    uint32_t w = ks[u][s >> 1];
+    asm volatile("" : "+v"(w));
+    return (int)((s & 1) ? w >> 16 : w & 0xFFFFu);
+  };
+  // A block with key scales out of the power's range: another power, if it is the largest or one that is not 0.  Returns
+  // whether that does not hold all of them; if it does, the zeros, also out of range, become what the power takes for 0.
+  const auto fit_scales = [&] {
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < KS / 2; ++i) top = max_pair(top, pair(ks[u][i]));
+    const int most = max((int)top.x, (int)top.y);
+    const auto small = [&] {
+      if (bias == 0) return false;
+      u16x2 least = {0xFFFF, 0xFFFF};  // less 1: a 0 is the largest
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < KS / 2; ++i) least = min_pair(least, pair(ks[u][i]) - (u16x2){1, 1});
+      return __builtin_amdgcn_ballot_w64(min((int)least.x, (int)least.y) < bias + kScaleLeast - 1) != 0;
+    };
+    const bool large = __builtin_amdgcn_ballot_w64(most - bias >= kScaleHigh) != 0;
+    bool split = false;
+    if (large || small()) {
+      bias = __builtin_amdgcn_readfirstlane(max((int)(wave_max((uint32_t)most) >> 7) - kScaleSet, 0) << 7);
+      set_scales((bias >> 7) - 112);
+      split = small();
+    }
+    if (!split) {
+      const u16x2 zero = {(unsigned short)bias, (unsigned short)bias};
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < KS / 2; ++i) ks[u][i] = __builtin_bit_cast(uint32_t, max_pair(pair(ks[u][i]), zero));
+    }
+    return split;
+  };
+  // The scores of a block whose key scales no power holds: those that one does at a time, from the largest down, and the
+  // products summed in fp32 at the scores' power.
+  const auto apart = [&](f32x4 (&xs)[2][NR]) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
+    int below = 0x8000;  // above the bits of the scales that are left
+    while (true) {
+      int left = 0;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const int v = scale_of(u, s);
+          left = max(left, v < below ? v : 0);
+        }
+      left = __builtin_amdgcn_readfirstlane((int)wave_max((uint32_t)left));
+      if (left == 0) break;
+      const int power = max((left >> 7) - kScaleSet, 0);
+      const int from = power == 0 ? 0 : (power << 7) + kScaleLeast;
+      const float weight = __builtin_amdgcn_ldexpf(1.0f, power - (bias >> 7));
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+          for (int s = 0; s < KS; ++s) {
+            const int v = scale_of(u, s);
+            const uint16_t bits = v < below && v >= from ? (uint16_t)((v - (power << 7)) << 3) : 0;
+            const _Float16 one = __builtin_bit_cast(_Float16, bits);
+            uint32_t w = kw[u][s];
+            asm volatile("" : "+v"(w));
+            Frag k = codes(w, magic);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              k.w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, k.w[i]) * (f16x2){one, one});
+            x = mfma(k, query(r, s), x);
+          }
+          xs[u][r] += x * weight;
+        }
+      }
+      below = from;
+    }
+  };
   for (int j = j0; j < j1; j += W) {
     const bool missing = page_of(j) < 0;
     const bool masked = missing || (j + 1) * kCacheBlock > all_seen;
     if (masked) {  // scales of slots that no row sees may be anything, of those that one does not see must be finite
+      const uint32_t held = bias == 0 ? 0 : (uint32_t)(bias + (kScaleSet << 7)) * 0x10001u;  // in the power's range
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        if (missing || j * kCacheBlock + u * 16 + n >= rg.keys) ks[u] = (u32x2){0, 0};
+        if (missing || j * kCacheBlock + u * 16 + n >= rg.keys) ks[u] = (u32x2){held, held};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           vs[u][i] = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(vs[u][i]), 0.0f, -kNoMax));
       }
     }
-    // Key scales to fp16: bf16 bits, with the exponent brought into range and the mantissa moved by 3 bits.
-    const u16x2 top2 = max_pair(max_pair(pair(ks[0].x), pair(ks[1].x)), max_pair(pair(ks[0].y), pair(ks[1].y)));
-    const int most = max((int)top2.x, (int)top2.y);
-    if (__builtin_amdgcn_ballot_w64(most - bias >= kScaleHigh) != 0 ||
-        (bias > 0 && __builtin_amdgcn_ballot_w64(most - bias >= kScaleLow) == 0)) {
-      bias = __builtin_amdgcn_readfirstlane(max((int)(wave_max((uint32_t)most) >> 7) - kScaleSet, 0) << 7);
-      set_scales((bias >> 7) - 112);
+    // Key scales to fp16: bf16 bits, with the exponent brought into range and the mantissa moved by 3 bits.  One
+    // comparison finds the scales on both sides of the range: those below wrap to large numbers.
+    const auto in_range = [&](u16x2 (&t)[2][KS / 2]) {
+      const u16x2 off = {(unsigned short)(bias + kScaleLeast), (unsigned short)(bias + kScaleLeast)};
+      u16x2 top = {0, 0};
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < KS / 2; ++i) {
+          t[u][i] = pair(ks[u][i]) - off;
+          top = u == 0 && i == 0 ? t[u][i] : max_pair(top, t[u][i]);
+        }
+      return __builtin_amdgcn_ballot_w64(max((int)top.x, (int)top.y) >= kScaleHigh - kScaleLeast) == 0;
+    };
+    u16x2 scales[2][KS / 2];
+    bool split = false;
+    if (!__builtin_expect(in_range(scales), true)) {
+      split = fit_scales();
+      in_range(scales);
     }
-    const u16x2 off = {(unsigned short)bias, (unsigned short)bias};
     f32x4 xs[2][NR];
+    if (__builtin_expect(split, false)) {
+      apart(xs);
+    } else {
+      const u16x2 eight = {8, 8}, least = {8 * kScaleLeast, 8 * kScaleLeast};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f16x2 sc[KS / 2];
+      for (int u = 0; u < 2; ++u) {
+        f16x2 sc[KS / 2];
 #pragma unroll
-      for (int i = 0; i < KS / 2; ++i)
-        sc[i] = __builtin_bit_cast(f16x2, __builtin_elementwise_sub_sat(pair(ks[u][i]), off) << 3);
+        for (int i = 0; i < KS / 2; ++i) sc[i] = __builtin_bit_cast(f16x2, scales[u][i] * eight + least);
 #pragma unroll
-      for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
+        for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const _Float16 one = sc[s >> 1][s & 1];
-        Frag k = codes(kw[u][s], magic);
+        for (int s = 0; s < KS; ++s) {
+          const _Float16 one = sc[s >> 1][s & 1];
+          Frag k = codes(kw[u][s], magic);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          k.w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, k.w[i]) * (f16x2){one, one});
+          for (int i = 0; i < 4; ++i)
+            k.w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, k.w[i]) * (f16x2){one, one});
 #pragma unroll
-        for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, query(r, s), xs[u][r]);
+          for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, query(r, s), xs[u][r]);
+        }
       }
     }
     // (after the last block, that block once more: no branch, so the registers stay in place)

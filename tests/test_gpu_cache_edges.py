@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+import cache_cases as cc
 import test_gpu_cache as T
 from oracle import cache_oracle as c
 from paper_2608_03276_amd import binding as B
@@ -106,3 +107,22 @@ def test_attention_scores_beyond_fp32(gpu_lib, d, T_, n):
                 ref, want, mag = c.attend(finite[0, t, h], k, v, np.arange(n) <= n - T_ + t, 1.0)
                 assert abs(l - want) <= 2.0 ** -10, (tag, l, want)
                 assert np.all(np.abs(got - ref) <= mag * 2.0 ** -8.5 + 2.0 ** -8 * np.abs(ref) + n * 2.0 ** -30 * np.abs(v).max()), tag
+
+
+# ------------------------------------------------------------------------------ key scales
+@pytest.mark.parametrize("shape", range(len(cc.SHAPES)))
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind", cc.KINDS)
+def test_attention_contents(gpu_lib, kind, d, shape):
+    """Strong and weak groups of channels, blocks of different power, tokens of very large keys, scores far from 0: within
+    what the arithmetic allows (cache_cases.py), for each form of the kernel."""
+    Hq, Hkv, lens, new, most = cc.SHAPES[shape]
+    s = T.Setup(80 + shape, 1, Hq, Hkv, d, 64, lens)
+    q, scale = cc.fill(s, kind, sum(new))
+    s.upload()
+    out, lse = T.attend(s, q, new, scale, max_len=most)
+    out, lse = T.f64(out)[0], T.f64(lse)[0]
+    for row, hq, bound in cc.rows(s, new, q, scale):
+        ref, want, tol, tol_lse = bound
+        assert cc.accepts(out[row, hq], lse[hq, row], bound), (
+            row, hq, float(np.max(np.abs(out[row, hq] - ref) / np.maximum(tol, 1e-300))), lse[hq, row], want, tol_lse)
