@@ -632,6 +632,9 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache_merge(CacheAttnArgs a) 
 
 }  // namespace
 
+constexpr int64_t kWhole = 4096, kCus = 256;
+constexpr int64_t kStreamed = 256 << 20;  // bytes of a cache that the chip's caches do not hold
+
 // Chunks: merging costs a launch (4 us) and, for each row and chunk, 4 d + 8 bytes written and read.
 //  - Rows of one or two tiles (decoding, drafts): chunks of 4096 tokens where the (sequence, head) pairs occupy
 //    every CU (32 sequences of 8 heads and 2049 to 2548 tokens: 27.2 us whole, 29.9 in chunks of 640); fewer pairs
@@ -652,7 +655,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache_merge(CacheAttnArgs a) 
 CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
                      int32_t max_len) {
   constexpr int64_t kUnit = 128;  // tokens: a block for each of four waves
-  constexpr int64_t kLeast = 512, kWhole = 4096, kWorkgroups = 1024, kCus = 256;
+  constexpr int64_t kLeast = 512, kWorkgroups = 1024;
   CachePlan p;
   const int64_t rows = (int64_t)(Hq / Hkv) * max_new;
   p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
@@ -683,7 +686,7 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
   const int64_t partials = finest == 1 ? 0 : std::min(heads * rows * finest, 128 * kWorkgroups + 32 * heads * whole);
   p.waves = p.tiles == 1 && p.chunks == 1 && units <= 2 * kCus ? 8 : 4;
   p.once = p.row_groups == 1 &&
-           (double)heads * max_len * (double)(cache_block_bytes(head_dim) / kCacheBlock) > (double)(256 << 20);
+           (double)heads * max_len * (double)(cache_block_bytes(head_dim) / kCacheBlock) > (double)kStreamed;
   p.stat_off = 0;
   p.o_off = ((size_t)partials * sizeof(float2) + 255) / 256 * 256;
   p.total = p.o_off + (size_t)partials * head_dim * sizeof(float);
@@ -694,8 +697,10 @@ namespace {
 
 template <int D, int NR, int W>
 void launch_part(const CacheAttnArgs& a, dim3 grid, hipStream_t stream) {
-  if (a.once)
-    hipLaunchKernelGGL((k_cache_attention<D, NR, W, true>), grid, dim3(64 * W), 0, stream, a);
+  // (eight waves: at most 2 kCus whole sequences, which at d = 64 are never that many bytes)
+  constexpr bool kMayStream = W == 4 || 2 * kCus * kWhole * (CacheBlock<D>::kBytes / kCacheBlock) > kStreamed;
+  if (kMayStream && a.once)
+    hipLaunchKernelGGL((k_cache_attention<D, NR, W, kMayStream>), grid, dim3(64 * W), 0, stream, a);
   else
     hipLaunchKernelGGL((k_cache_attention<D, NR, W, false>), grid, dim3(64 * W), 0, stream, a);
 }

@@ -126,3 +126,27 @@ def test_attention_contents(gpu_lib, kind, d, shape):
         ref, want, tol, tol_lse = bound
         assert cc.accepts(out[row, hq], lse[hq, row], bound), (
             row, hq, float(np.max(np.abs(out[row, hq] - ref) / np.maximum(tol, 1e-300))), lse[hq, row], want, tol_lse)
+
+
+# ------------------------------------------------------------------------------ streamed caches
+@pytest.mark.parametrize("R,T_", [(1, 1), (8, 4), (8, 5)])
+def test_attention_of_a_large_cache_of_small_heads(gpu_lib, R, T_):
+    """d = 64 and a length bound by which the cache is streamed, with one to four tiles."""
+    lens, new = [9000, 700, 17, 5000], [T_, min(T_, 2), T_, 1]
+    s = T.Setup(73, 1, 2 * R, 2, 64, 64, lens, cols=1 << 14)
+    q = s.rows(sum(new), 2 * R)
+    out, lse = T.attend(s, q, new, 0.1, max_len=1 << 20, max_new=T_)
+    T.check_attention(s, q, new, T.f64(out), T.f64(lse), 0.1, heads=[1])
+    few, lse_few = T.attend(s, q, new, 0.1, max_len=9000, max_new=T_)
+    T.check_attention(s, q, new, T.f64(few), T.f64(lse_few), 0.1, heads=[1])
+
+
+@pytest.mark.parametrize("most", [4096, 2048])
+def test_attention_of_many_whole_sequences(gpu_lib, most):
+    """Eight waves a sequence, streamed (496 pairs of up to 4096 tokens are 284 MB) and not."""
+    lens = [2500, 4, 0, 700] + [1 + i % 40 for i in range(58)]
+    lens[0] = min(lens[0], most)
+    s = T.Setup(74, 1, 16, 8, 128, 64, lens, cols=4096 // 64)
+    q = s.rows(len(lens), 16)
+    out, lse = T.attend(s, q, [1] * len(lens), 0.1, max_len=most)
+    T.check_attention(s, q, [1] * len(lens), T.f64(out), T.f64(lse), 0.1, only=[0, 1, 2, 3, 30, 61], heads=[0, 7])
