@@ -656,6 +656,7 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
                      int32_t max_len) {
   constexpr int64_t kUnit = 128;  // tokens: a block for each of four waves
   constexpr int64_t kLeast = 512, kWorkgroups = 1024;
+  constexpr int64_t kMost = 8;    // workgroups a CU
   CachePlan p;
   const int64_t rows = (int64_t)(Hq / Hkv) * max_new;
   p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
@@ -666,7 +667,7 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
   if (p.tiles == 4) {
     int64_t least = 0;
     chunks = 0;
-    for (int64_t w = 0; w <= 8; ++w) {  // whole, and the most chunks of w workgroups a CU
+    for (int64_t w = 0; w <= kMost; ++w) {  // whole, and the most chunks of w workgroups a CU
       const int64_t c = w == 0 ? 1 : std::min(finest, w * kCus / units);
       if (c <= chunks) continue;
       const int64_t each = (units * c + kCus - 1) / kCus, blocks = each * ((n + c * kCacheBlock - 1) / (c * kCacheBlock));
@@ -681,9 +682,11 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
   }
   p.chunk = (int32_t)(((n + chunks - 1) / chunks + kUnit - 1) / kUnit * kUnit);
   p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
-  // Partial rows: up to 32 a pair in chunks of kWhole, up to 64 (kWorkgroups + units) in the fill.  The bound
-  // grows with every argument, so a buffer for the longest call serves the others.
-  const int64_t partials = finest == 1 ? 0 : std::min(heads * rows * finest, 128 * kWorkgroups + 32 * heads * whole);
+  // Partial rows, heads * rows * chunks.  One or two tiles: rows <= 32 and chunks <= max(whole, kWorkgroups / heads + 1), so
+  // at most 32 (kWorkgroups + heads * whole).  Four: heads * rows <= 64 units and, where there are chunks, chunks <=
+  // kMost * kCus / units.  Both bounds in one, which grows with every argument, so a buffer for the longest call serves the others.
+  static_assert(32 * kWorkgroups <= 64 * kMost * kCus);
+  const int64_t partials = finest == 1 ? 0 : std::min(heads * rows * finest, 64 * kMost * kCus + 32 * heads * whole);
   p.waves = p.tiles == 1 && p.chunks == 1 && units <= 2 * kCus ? 8 : 4;
   p.once = p.row_groups == 1 &&
            (double)heads * max_len * (double)(cache_block_bytes(head_dim) / kCacheBlock) > (double)kStreamed;
