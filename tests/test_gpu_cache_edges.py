@@ -150,3 +150,60 @@ def test_attention_of_many_whole_sequences(gpu_lib, most):
     q = s.rows(len(lens), 16)
     out, lse = T.attend(s, q, [1] * len(lens), 0.1, max_len=most)
     T.check_attention(s, q, [1] * len(lens), T.f64(out), T.f64(lse), 0.1, only=[0, 1, 2, 3, 30, 61], heads=[0, 7])
+
+
+# ------------------------------------------------------------------------------ outputs on the queries, a second eviction
+@pytest.mark.parametrize("lens,new", [([90, 41], [3, 2]), ([9000, 70], [17, 1]), ([300], [100]), ([2000, 1], [1, 1])])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_in_place_is_right(gpu_lib, d, lens, new):
+    """Outputs written over the queries, whole and in chunks, against the oracle."""
+    s = T.Setup(75, 1, 8, 2, d, 64, lens)
+    q = s.rows(sum(new), 8)
+    rows, lse = T.bf16(q[0]).cuda(), torch.full((8, sum(new)), -7.0, device="cuda")
+    step = B.Step(sum(new), max(new), torch.from_numpy(T.offsets_of(new)).cuda())
+    B.tp_cache_attention(s.dims, s.cache, step, rows, 0.1, max(lens), rows, lse)
+    got, gl = T.f64(rows), T.f64(lse)
+    for row, hq, bound in cc.rows(s, new, q, 0.1):
+        assert cc.accepts(got[row, hq], gl[hq, row], bound), (row, hq)
+
+
+def codes_and_scales(s, b, layer, head, n):
+    """Codes and scales of a sequence's first n tokens: keys int [n][d], float [n][d / 32], values int [n][d], float [n]."""
+    d, out = s.d, [[], [], [], []]
+    pages = s.dev.cpu().numpy()
+    kb, ks, vb, vs = c.places(d)
+    for t in range(0, n, 32):
+        page, j, _ = c.place_of(s.table[b], s.num, s.page, t)
+        block = pages[layer, page, head, j]
+        bits = block[32 * d:34 * d].copy().view(np.uint16).astype(np.uint32) << 16
+        for part, x in zip(out, ((block[kb] >> ks & 15).astype(int) - 8, bits.view(np.float32).reshape(32, -1),
+                                 (block[vb] >> vs & 15).astype(int) - 8, block[34 * d:].copy().view(np.float32))):
+            part.append(x)
+    return [np.concatenate(x)[:n].astype(np.float64) for x in out]
+
+
+@pytest.mark.parametrize("d,page", [(64, 32), (128, 64)])
+def test_second_eviction_keeps_the_codes(gpu_lib, d, page):
+    """Rows read back, evicted again and loaded: the kept tokens' codes are those that were held.  A scale is 1/7 of the
+    rounded 7 scale: off by at most 2^-8 of itself for values, by that and its own rounding, 2^-8 more, for keys (the
+    largest code of a group or row is 7)."""
+    L, Hq, Hkv, lens, budget = 2, 4, 2, [300, 77], [45, 45]
+    s = T.Setup(76, L, Hq, Hkv, d, page, lens)
+    n = sum(lens)
+    step = B.Step(n, max(lens), torch.from_numpy(T.offsets_of(lens)).cuda())
+    B.tp_cache_append(s.dims, s.cache, step, T.bf16(s.rows(n, Hkv, 3.0)).cuda(), T.bf16(s.rows(n, Hkv, 0.2)).cuda())
+    before = {(b, l, h): codes_and_scales(s, b, l, h, lens[b]) for b in range(2) for l in range(L) for h in range(Hkv)}
+    k = torch.empty((L, Hkv, n, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    back = B.Batch([0, 300, 377], [0, 8, 16])
+    B.tp_cache_read(s.dims, s.cache, back, k, v)
+    qg = T.bf16(s.rng.normal(size=(L, Hq, 16, d))).cuda()
+    bufs = B.evict_fused(s.dims, back, qg, k, v, softmax_scale=0.125, pool_k=5, qfmt=B.TP_QFMT_INT, bits=4, keep_budget=45)
+    B.tp_cache_load(s.dims, s.cache, bufs.kept_offsets, bufs.k_c, bufs.v_q_c, bufs.scales_c, 4)
+    idx = bufs.kept_idx.view(L, Hkv, 90).cpu().numpy()
+    for (b, l, h), was in before.items():
+        kept = idx[l, h, 45 * b:45 * (b + 1)]
+        now = codes_and_scales(s, b, l, h, 45)
+        assert np.array_equal(now[0], was[0][kept]) and np.array_equal(now[2], was[2][kept]), (b, l, h)
+        assert np.all(np.abs(now[1] / was[1][kept] - 1) <= 2.0 ** -7 * (1 + 2.0 ** -8)), (b, l, h)
+        assert np.all(np.abs(now[3] / was[3][kept] - 1) <= 2.0 ** -8 * (1 + 2.0 ** -8)), (b, l, h)
