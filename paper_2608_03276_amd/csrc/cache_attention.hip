@@ -10,16 +10,17 @@
 // query row from the scores to the output and the weights never leave their registers:
 //   scores  S^T = K Q^T: codes times their group's scale, exact in fp16, one chain of products through the groups;
 //   output  O^T += V^T P^T, with the values' scales multiplied into the weights P.
-// Codes become fp16 operands by bit operations on pairs: 0x6400 | u is 1024 + u for a 4-bit number u = c + 8,
-// and one packed fp16 operation more gives c exactly.  fp16 holds queries exactly once a row is brought near
-// 2^14 by a power of two (a bf16 number has 8 significant bits, fp16 11; what lies 2^28 below the row's largest
-// channel is off by 2^-39 of that one), and keeps the weights' rounding, 2^-11, below the output's (with bf16
-// operands the output's error was 1.4 times that of its own rounding).
+// Codes become fp16 operands by bit operations on pairs: 0x6400 | u is 1024 + u for a 4-bit number u = c + 8, and
+// one packed fp16 operation more gives c exactly (a published way: Y. J. Kim et al., "Who Says Elephants Can't Run:
+// Bringing Large Scale MoE Models into Cloud Scale Production", 2022; here with an offset of 8).  fp16 holds
+// queries exactly once a row is brought near 2^14 by a power of two (a bf16 number has 8 significant bits, fp16 11;
+// what lies 2^28 below the row's largest channel is off by 2^-39 of that one), and keeps the weights' rounding,
+// 2^-11, below the output's (with bf16 operands the output's error was 1.4 times that of its own rounding).
 //
 // Measured at d = 128: one row tile is bound by HBM (64 sequences of 6K to 32K tokens, 64 query heads: 1.16 GB in
-// 222 us, 5.2 TB/s; two of 262144 and 131073: 440 MB in 76 us), four by the vector ALU (chunks of 1024 and 300
-// tokens against 17333 and 4096, 32 query heads: 302 GFLOP in 329 us).  Of 270 vector instructions a block with
-// one tile, 461 with four, 176 turn codes into operands.
+// 223 us, 5.2 TB/s; two of 262144 and 131073: 440 MB in 77 us), four by the vector ALU (chunks of 1024 and 300
+// tokens against 17333 and 4096, 32 query heads: 302 GFLOP in 325 us).  Of 272 vector instructions a block with
+// one tile, 446 with four, 176 turn codes into operands.
 //
 // The running reference m of a row bounds the weights that are rounded, p * scale of the value, not p alone:
 // p = exp2(x - m) and the sum of the p's are fp32, in which the reference may be anywhere.
@@ -646,12 +647,23 @@ constexpr int64_t kStreamed = 256 << 20;  // bytes of a cache that the chip's ca
 //    21.9 and 17.6, and with lengths down to a tenth of that 18.8 and 17.3; two tiles: 8 of 1024 12.8 and 14.2, 20
 //    of 1024 18.2 and 15.1).
 //    Whole sequences of at most two workgroups a CU take eight waves (those 32 sequences: 26.2 us with four, 23.4
-//    with eight, the append before it 5.8 of them; 64 of 6K to 32K tokens in chunks: 235 and 249).
+//    with eight, the append before it 5.8 of them; 64 of their lengths: 35.0 and 36.3; 64 of 6K to 32K tokens in
+//    chunks: 235 and 249).
 //  - Four tiles (prompts): the least cost of the busiest CU, in blocks of the cache: those of its workgroups (0.3 us
 //    each; with one workgroup a CU half as much again), and, where there are chunks, 16 a workgroup for its partial
 //    rows and 6 for the merge.  Measured with 32 query, 8 KV heads: 256 new tokens against 4096 in 4 chunks 36 us, in
 //    2 40, in 8 50; 512 against 1024 whole 22, in 2 29; 1024 against 4096 whole 83, in 2 100; 64 against 1024 in 2 18,
 //    whole 21.
+// All of this at d = 128.  At d = 64 a block takes two thirds of the time, and the same choices are the better ones (17
+// sequences of 2048 11.5 us whole, 13.0 split; 25 of 2600 13.7 and 17.2; those 32 with four waves 16.5, with eight 13.7;
+// 20 of 1024 with two tiles 12.1 whole, 14.2 split; 256 new against 4096 in 4 27.2, in 2 31.0, in 8 34.8; 64 against 1024
+// in 2 14.2, whole 16.6) but near a border (one sequence of 1024 9.1 split, 7.8 whole; 8 of 1400 9.4 and 8.9).
+//
+// max_len and max_new stand for every sequence, and a call pays for what they allow beyond what its sequences hold: those 32
+// sequences, alone, take 19 us with a bound of 2548 or 4096, 32 with 8192 (chunks: four waves and a merge; streamed), 55
+// with 32768, 64 with 131072 (workgroups that end at once).  Decoding sequences beside a prompt's chunk take the chunk's
+// row groups and are not split: 15 of 8192 beside 1024 new tokens against 4096 199 us, apart 46 and 84; 63 of them 538,
+// apart 149 and 84 (bound 32768).
 CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
                      int32_t max_len) {
   constexpr int64_t kUnit = 128;  // tokens: a block for each of four waves
@@ -684,7 +696,8 @@ CachePlan cache_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32
   p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
   // Partial rows, heads * rows * chunks.  One or two tiles: rows <= 32 and chunks <= max(whole, kWorkgroups / heads + 1), so
   // at most 32 (kWorkgroups + heads * whole).  Four: heads * rows <= 64 units and, where there are chunks, chunks <=
-  // kMost * kCus / units.  Both bounds in one, which grows with every argument, so a buffer for the longest call serves the others.
+  // kMost * kCus / units.  Both bounds in one, which grows with every argument, so a buffer for the longest call serves
+  // the others.
   static_assert(32 * kWorkgroups <= 64 * kMost * kCus);
   const int64_t partials = finest == 1 ? 0 : std::min(heads * rows * finest, 64 * kMost * kCus + 32 * heads * whole);
   p.waves = p.tiles == 1 && p.chunks == 1 && units <= 2 * kCus ? 8 : 4;

@@ -7,9 +7,9 @@
 // one workgroup of the launch, so nothing races.  Everything that a workgroup loads hangs on the sequence's
 // offsets and length alone, but for the angles (on the positions) and the old values (on the page).
 //
-// Bound by HBM (d = 128): 13107 kept tokens of 32 layers and 8 heads into pages in 300 us (6.2 TB/s) and back in 428
-// (4.4, four fifths of it writes); 12290 new tokens of 64 query and 8 KV heads in 105 us (4.5 TB/s).  A decoding
-// step's append is latency: 64 sequences in 5.9 us.
+// Bound by HBM (d = 128): 13107 kept tokens of 32 layers and 8 heads into pages in 300 us (464 bytes a token and head,
+// 5.2 TB/s) and back in 428 (652 bytes, 5.1 TB/s, four fifths of it writes); 12290 new tokens of 64 query and 8 KV
+// heads in 105 us (4.5 TB/s).  A decoding step's append is latency: 64 sequences in 5.9 us.
 #include "cache_block.h"
 #include "quant_row.h"
 
@@ -426,7 +426,7 @@ __device__ inline void store16(uint4* p, const uint4& x) {
     *p = x;
 }
 
-// ONCE: the rows are more than the chip's caches hold, so no later kernel finds them there (8 layers and heads, 27000
+// ONCE: the rows are more than the chip's caches hold, so no later kernel finds them there (8 layers and heads, 29755
 // tokens: 254 us, 240 with it).
 template <int D, bool ONCE>
 __global__ __launch_bounds__(kRowsThreads) void k_cache_read(CacheReadArgs a) {
