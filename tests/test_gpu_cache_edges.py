@@ -207,3 +207,89 @@ def test_second_eviction_keeps_the_codes(gpu_lib, d, page):
         assert np.array_equal(now[0], was[0][kept]) and np.array_equal(now[2], was[2][kept]), (b, l, h)
         assert np.all(np.abs(now[1] / was[1][kept] - 1) <= 2.0 ** -7 * (1 + 2.0 ** -8)), (b, l, h)
         assert np.all(np.abs(now[3] / was[3][kept] - 1) <= 2.0 ** -8 * (1 + 2.0 ** -8)), (b, l, h)
+
+
+# ------------------------------------------------------------------------------ batches, pages, captured calls
+def test_largest_batch(gpu_lib):
+    """65535 sequences of one token, every page its own: attention gives each its value back, bit for bit as read."""
+    n = 65535
+    dims = B.dims(1, 2, 1, 64)
+    pages = torch.zeros(n * B.tp_cache_page_bytes(dims, 32), dtype=torch.uint8, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    table = torch.randperm(n, device="cuda", generator=g).to(torch.int32).view(n, 1)
+    cache = B.Cache(dims, pages, table, torch.ones(n, dtype=torch.int32, device="cuda"), 32)
+    k, v = (torch.randn((n, 1, 64), device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((n, 2, 64), device="cuda", generator=g).to(torch.bfloat16)
+    B.tp_cache_append(dims, cache, B.Step(n), k, v)
+    out, lse = torch.full_like(q, -7.0), torch.zeros((2, n), device="cuda")
+    B.tp_cache_attention(dims, cache, B.Step(n), q, 0.125, 32, out, lse)
+    few = [0, 1, 31, 4095, 40000, 65471, 65534]
+    back = B.Cache(dims, pages, table[few].contiguous(), torch.ones(len(few), dtype=torch.int32, device="cuda"), 32)
+    kk, vv = (torch.empty((1, 1, len(few), 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.tp_cache_read(dims, back, B.Batch(list(range(len(few) + 1))), kk, vv)
+    held = vv[0, 0].float()
+    for h in range(2):  # one weight, rounded to fp16 once and divided by in fp32: 2^-11, and bf16's 2^-8
+        assert bool(((out[few, h].float() - held).abs() <= held.abs() * (2.0 ** -8 + 2.0 ** -10.9)).all())
+        want = 0.125 * (q[few, h].float() * kk[0, 0].float()).sum(1)
+        # keys read back are rounded to bf16: 2^-8 of each of 64 terms, of at most 3 * 4 * 0.125 each
+        assert bool(((lse[h, few] - want).abs() <= 64 * 1.5 * 2.0 ** -8).all())
+    scale = (v.float().abs().amax(-1, keepdim=True) / 7)
+    assert bool(((out.float() - v.float()).abs() <= scale * (0.5 + 7 * 2.0 ** -7)).all())  # every row: half a step
+
+
+def test_shared_pages(gpu_lib):
+    """A prefix that sequences share is listed by all of them; a page may also come twice in one sequence."""
+    s = T.Setup(77, 1, 8, 2, 128, 32, [200, 200, 96, 64])
+    s.table[1, :5] = s.table[0, :5]
+    s.table[2, 2] = s.table[2, 0]
+    s.upload()
+    q = s.rows(4, 8)
+    q[0, 1] = q[0, 0]
+    out, lse = T.attend(s, q, [1] * 4, 0.1)
+    got, gl = T.f64(out)[0], T.f64(lse)[0]
+    for row, hq, bound in cc.rows(s, [1] * 4, q, 0.1):
+        assert cc.accepts(got[row, hq], gl[hq, row], bound), (row, hq)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_load_leaves_out_missing_pages(gpu_lib, d):
+    s = T.Setup(78, 2, 2, 2, d, 32, [100, 64, 33])
+    s.table[0, 1], s.table[1, 0], s.table[2, 1] = -1, s.num, 2 ** 31 - 1
+    s.upload()
+    off = [0, 100, 164, 197]
+    k = c.to_bf16(s.rng.normal(size=(2, 2, 197, d)))
+    v = T.bf16(s.rng.normal(size=(2, 2, 197, d))).cuda()
+    scales = torch.empty((2, 2, 197), device="cuda")
+    v_q = torch.empty((2, 2, 197, d // 2), dtype=torch.uint8, device="cuda")
+    B.tp_quantize_v_scales(s.dims, B.Batch([0, 197]), v, B.TP_QFMT_INT, 4, scales, v_q)
+    B.tp_cache_load(s.dims, s.cache, off, T.bf16(k).cuda(), v_q, scales, 4)
+    vv = T.f64(v)
+    for b in range(3):
+        for t in range(off[b + 1] - off[b]):
+            for l in range(2):
+                for h in range(2):
+                    s.write(b, t, l, h, c.quantise_key(k[l, h, off[b] + t]), c.quantise_value(vv[l, h, off[b] + t]))
+    s.check_pages()
+
+
+@pytest.mark.parametrize("given", ["current", "stream", "handle"])
+def test_captured_without_a_workspace(gpu_lib, given):
+    """A captured call that makes its own scratch, on the capturing stream: replays against eager calls."""
+    s = T.Setup(79, 1, 8, 2, 64, 32, [3000, 500])
+    side, step = torch.cuda.Stream(), B.Step(2)
+    rows, out = torch.zeros((2, 8, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 8, 64), dtype=torch.bfloat16, device="cuda")
+    stream = {"current": None, "stream": side, "handle": side.cuda_stream}[given]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        B.tp_cache_attention(s.dims, s.cache, step, rows, 0.125, 3008, out, stream=stream)
+    for i in range(4):
+        q = s.rows(2, 8)
+        rows.copy_(T.bf16(q[0]))
+        want, _ = T.attend(s, q, [1, 1], 0.125)
+        other = [torch.full((1 << 20,), i, device="cuda") for _ in range(3)]  # the program's own memory
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0])
+        assert all(bool((x == i).all()) for x in other)
