@@ -45,6 +45,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 // ends below 2^16): most blocks skip the rescaling and the reduction across lanes, and weights down to
 // 2^-22 of the largest are normal fp16 numbers.
 constexpr float kSet = 8.0f, kLimit = 16384.0f;
+// A reference is one fp32 number, so the exponent x - m is off by half its unit: 4 at 2^26, between kSet and kLimit.
+// Scores beyond that (where one rounding of a score changes a weight by 2^4) count as infinities: a reference starts at
+// -2^26, which leaves keys below that no weight, and one above 2^26 makes the row NaN.
+constexpr float kFar = 0x1p26f;
 // Scales below 2^-60 count as that in the reference, and sums of p above 2^74 raise it too, so that tokens
 // with tiny or zero values cannot overflow the sum.
 constexpr float kLeastScale = 0x1p-60f;
@@ -141,11 +145,11 @@ __device__ inline int64_t partial_row(const CacheAttnArgs& a, int chunk, int b, 
 }
 
 // CH channels of a row from c0: the sum of weighted values over the sum of weights (st.y), and the log-sum-exp.  The sum
-// is 0 where no key was seen, and NaN (with every channel's) where a score was +infinity or NaN.
+// is 0 where no key was seen; a row with a score of +infinity (its reference is beyond kFar) or NaN is NaN throughout.
 template <int CH>
 __device__ inline void store_output(const CacheAttnArgs& a, int layer, int64_t token, int hq, int c0, const float (&o)[CH],
                                     const float2& st) {
-  const float inv = st.y == 0.0f ? 0.0f : 1.0f / st.y;
+  const float sum = st.x > kFar ? NAN : st.y, inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   uint16_t* to = a.o.data + layer * a.o.layer + token * a.o.token + hq * a.o.head + c0;
   typedef __bf16 bf16s __attribute__((ext_vector_type(CH)));
   bf16s v;
@@ -154,7 +158,7 @@ __device__ inline void store_output(const CacheAttnArgs& a, int layer, int64_t t
   *(bf16s*)to = v;
   if (a.lse != nullptr && c0 == 0)
     a.lse[((int64_t)layer * a.Hq + hq) * a.s.total + token] =
-        st.y == 0.0f ? -INFINITY : (st.x + __builtin_amdgcn_logf(st.y)) * kLn2;
+        sum == 0.0f ? -INFINITY : (st.x + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // NR tiles of 16 rows, W waves.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave it out).
@@ -263,7 +267,7 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
   float m[NR], l[NR];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    m[r] = kNoMax;
+    m[r] = -kFar;
     l[r] = 0.0f;
 #pragma unroll
     for (int x = 0; x < ND; ++x) acc[r][x] = (f32x4){0, 0, 0, 0};

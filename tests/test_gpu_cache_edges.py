@@ -109,6 +109,62 @@ def test_attention_scores_beyond_fp32(gpu_lib, d, T_, n):
                 assert np.all(np.abs(got - ref) <= mag * 2.0 ** -8.5 + 2.0 ** -8 * np.abs(ref) + n * 2.0 ** -30 * np.abs(v).max()), tag
 
 
+@pytest.mark.parametrize("lens,new", [([1, 70], [1, 1]), ([1, 700], [1, 20]), ([33, 9000], [5, 6])])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_scores_of_any_size(gpu_lib, d, lens, new):
+    """Rows whose keys all have one score, of magnitudes from 1 to 2^40: their mean up to 2^26 / log2(e), beyond that as for
+    infinities.  The scores are exact; the log-sum-exp's error is 2^-22 of it and of the score, and 2^-14."""
+    s = T.Setup(70, 1, 4, 2, d, 64, lens)
+    blocks = s.pages.reshape(-1, c.block_bytes(d))
+    words = blocks[:, :16 * d].reshape(len(blocks), 32, 4, d // 32, 4)
+    words[:] = 0x88
+    words[:, :, 0, 0, 0] = 0x8C  # channel 0: 4
+    blocks[:, 32 * d:34 * d] = c.bf16_bits(np.full((len(blocks), d), 0.25)).view(np.uint8).reshape(len(blocks), -1)
+    s.upload()
+    held = [[c.held(s.pages, d, s.table[b], 64, 0, h, lens[b])[1] for h in range(2)] for b in range(2)]
+    for x in (1.0, 2.0 ** 20, 1.375 * 2.0 ** 25, 1.40625 * 2.0 ** 25, 1.5 * 2.0 ** 25, 2.0 ** 31, 1.125 * 2.0 ** 37, 2.0 ** 40):
+        for sign in (1, -1):
+            q = np.zeros((1, sum(new), 4, d))
+            q[..., 0] = sign * x
+            out, lse = T.attend(s, q, new, 1.0)
+            out, lse = T.f64(out)[0], T.f64(lse)[0]
+            far = x * 1.4426950408889634 > 2.0 ** 26
+            for row in range(sum(new)):
+                b, t = (0, row) if row < new[0] else (1, row - new[0])
+                n = lens[b] - new[b] + t + 1
+                for h in range(4):
+                    tag, got, l = (sign * x, b, t, h), out[row, h], lse[h, row]
+                    if far and sign > 0:
+                        assert np.isnan(l) and np.isnan(got).all(), (tag, l)
+                    elif far:
+                        assert l == -math.inf and not got.any(), (tag, l)
+                    else:
+                        v = held[b][h // 2][:n]
+                        mean, mag = v.mean(0), np.abs(v).mean(0)
+                        want = sign * x + math.log(n)
+                        assert abs(l - want) <= 2.0 ** -21 * x + 2.0 ** -14 + 2.0 ** -22 * abs(want), (tag, l, want)
+                        tol = mag * (2.0 ** -10.9 + 2.0 ** -14) + 2.0 ** -8 * np.abs(mean) + n * 2.0 ** -30 * np.abs(v).max()
+                        assert np.all(np.abs(got - mean) <= tol), tag
+
+
+def test_attention_of_a_far_first_block(gpu_lib):
+    """A block all of whose keys score far below 0, before ordinary ones, leaves nothing behind."""
+    s = T.Setup(69, 1, 4, 2, 128, 64, [40, 700])
+    q, scale = cc.fill(s, "massive", 2)
+    blocks = s.pages.reshape(-1, 2, s.page // 32, c.block_bytes(128))
+    for page, j in ((s.table[0, 0], 0), (s.table[1, 0], 0), (s.table[1, 3], 1)):
+        for h in range(2):
+            blk = blocks[page, h, j]
+            blk[:16 * 128].reshape(32, 4, 4, 4)[:] = 0x88
+            blk[:16 * 128].reshape(32, 4, 4, 4)[:, 0, 0, 0] = 0x81
+            blk[32 * 128:34 * 128] = c.bf16_bits(np.full(128, 2.0 ** 45)).view(np.uint8)
+    s.upload()
+    out, lse = T.attend(s, q, [1, 1], scale, max_len=700)
+    out, lse = T.f64(out)[0], T.f64(lse)[0]
+    for row, hq, bound in cc.rows(s, [1, 1], q, scale):
+        assert cc.accepts(out[row, hq], lse[hq, row], bound), (row, hq, lse[hq, row], bound[1])
+
+
 # ------------------------------------------------------------------------------ key scales
 @pytest.mark.parametrize("shape", range(len(cc.SHAPES)))
 @pytest.mark.parametrize("d", [64, 128])
