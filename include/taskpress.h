@@ -488,9 +488,9 @@ tp_status tp_cache_workspace_size(const tp_dims* dims, const tp_cache* cache, co
  * q, o rows of Hq heads; o may be q (the same data and strides).  o is rounded to bf16 once; lse fp32
  * [L][Hq][total], 4-byte aligned, or NULL.
  * max_len: at least every lens[b] (host; in [1, max_pages * page_tokens]); a longer sequence counts
- * as empty.  softmax_scale > 0, finite.  A score times log2(e) beyond 2^26 in magnitude, where fp32's unit is 8, counts
- * as an infinity: a key whose score is -infinity is not seen; a row that sees a key with a score of +infinity, or sees
- * any key and has a query that is not finite, gets o and lse NaN.
+ * as empty.  softmax_scale > 0, finite.  A score times log2(e) beyond 2^26 in magnitude (to within 200; fp32's unit is 8
+ * there) counts as an infinity: a key whose score is -infinity is not seen; a row that sees a key with a score of
+ * +infinity, or sees any key and has a query that is not finite, gets o and lse NaN.
  * workspace: device, >= tp_cache_workspace_size() bytes, 256-byte aligned (NULL if that is 0).
  * Every token of a sequence that has a page holds a key and a value (was loaded or appended); what lies
  * behind the sequence's last token may be anything.  A channel of a query that is 2^28 or more below its row's
