@@ -17,6 +17,8 @@
  *   tp_cache_append           new tokens' keys, rotated at their positions, and values.
  *   tp_cache_attention        the newest tokens' attention over the pages.
  *   tp_cache_read             tokens back as bf16 rows, to evict again.
+ * and the same on pages of 8-bit keys and values, integers or e4m3: tp_cache8_load, tp_cache8_append,
+ * tp_cache8_attention, tp_cache8_read.
  *
  * Conventions (every entry point):
  *  - Returns tp_status.  All arguments are validated on the host before any GPU
@@ -516,6 +518,79 @@ tp_status tp_cache_attention(const tp_dims* dims, const tp_cache* cache, const t
  */
 tp_status tp_cache_read(const tp_dims* dims, const tp_cache* cache, const tp_batch* batch, const int64_t* first,
                         void* k_out, void* v_out, void* stream);
+
+/* ------------------------------------------------------------------ the paged 8-bit cache
+ *
+ * The cache for evictions that quantise V to more than 4 bits or to e4m3: pages, page table, lengths, steps, rows
+ * and rotation as above, with 8-bit codes.  What is held of a token, per (layer, KV head), in the cache's qfmt, with
+ * Q = 127 (TP_QFMT_INT, codes c in [-127, 127]) or 448 (TP_QFMT_FP8_E4M3, codes c of OCP E4M3):
+ *   key    one fp32 scale for the block of 32 tokens that the token lies in, c = fl32(k / scale) rounded to the nearest
+ *          code (ties to even, at most Q; the sign of a zero is kept), from the bf16 key row (rotated, rounded to bf16).
+ *          With m the largest magnitude of the keys that a call writes into a block, the block's scale becomes fl32(m / Q)
+ *          if it has no tokens before the call's (or its scale is 0, or not a number that a call has written).  Otherwise its
+ *          scale is kept if that is >= fl32(m / Q), and if not becomes 2^n times itself, n the least that reaches fl32(m / Q),
+ *          and the codes of the tokens before the call's become c 2^-n, rounded to the nearest code.  So a key held is off by
+ *          less than a step of its block's scale (integers: 1/2 (1 + 1/2 + 1/4 + ...) of it, however often the scale rises;
+ *          e4m3: half a unit of its last place, and 2^-9 of the scale for numbers that became subnormal).
+ *   value  Eq. 2: the scale and codes of tp_quantize_v_scales with the cache's qfmt (8 bits).  tp_cache8_load
+ *          copies the eviction's, of any number of bits.
+ * The key and value held are c * scale: 260.5 bytes a token and head at d = 128, 132.5 at 64 (bf16 rows: 512, 256).
+ *
+ * pages: bytes [L][num_pages][Hkv][page_tokens / 32][64 d + 144], a block being key codes (32 d bytes), value codes (32 d),
+ * value scales (fp32 [32]), the key scale (fp32) and 12 bytes that are not used.  A code is held as the byte c + 128
+ * (TP_QFMT_INT) or as its E4M3 byte.  Of token t (0..31) and channel x:
+ *   keys    byte (t / 16) * 16 d + (x / 64) * 1024 + (x % 32 / 8 * 16 + t % 16) * 16 + (x / 32 % 2) * 8 + x % 8;
+ *   values  byte (x / 32) * 1024 + (t % 16 / 4 * 16 + x % 16) * 16 + (x / 16 % 2) * 8 + t / 16 * 4 + t % 4.
+ * Layer l's part starts at l * num_pages * Hkv * tp_cache8_page_bytes().  Any initial contents are allowed; what a call does
+ * not write keeps its value.
+ */
+typedef struct tp_cache8 {
+  tp_cache cache; /* as above, its pages in this format */
+  int32_t qfmt;   /* TP_QFMT_INT or TP_QFMT_FP8_E4M3 (TP_ERR_PARAM otherwise) */
+} tp_cache8;
+
+/* Bytes of one page of one (layer, KV head): page_tokens / 32 * (64 d + 144); 0 for arguments that no cache has
+ * (tp_last_error() says which).  Host only. */
+size_t tp_cache8_page_bytes(const tp_dims* dims, int32_t page_tokens);
+
+/*
+ * The compact cache of an eviction into the pages, as tp_cache_load: keys quantised as above, value codes and scales
+ * copied.  TP_QFMT_INT: v_q of `bits` in [2, 8] (rows of d / 2 bytes up to 4 bits, d beyond); TP_QFMT_FP8_E4M3: e4m3
+ * codes (none of them NaN), rows of d bytes, bits ignored.  The other arguments, limits and errors as tp_cache_load.
+ */
+tp_status tp_cache8_load(const tp_dims* dims, const tp_cache8* cache, const int64_t* kept_offsets, const void* k,
+                         const void* v_q, const float* scales, int32_t bits, void* stream);
+
+/*
+ * A step's new tokens into the pages, as tp_cache_append: keys rotated on the way, and with q their query rows rotated
+ * beside them.  Reads the scale and, where that rises, the earlier tokens' key codes of the block that the step begins in:
+ * these tokens hold keys (were loaded or appended).  A sequence that is cut back (lens lowered) keeps its last block's
+ * scale.  Arguments, limits and errors as tp_cache_append.
+ */
+tp_status tp_cache8_append(const tp_dims* dims, const tp_cache8* cache, const tp_step* step, const tp_rows* k,
+                           const tp_rows* v, const int32_t* positions, const tp_rope* rope, const tp_rows* q,
+                           const tp_rows* q_out, void* stream);
+
+/* Bytes of workspace tp_cache8_attention needs for these arguments (host only; may be 0).  Never falls when total,
+ * max_new, max_len or the batch grows. */
+tp_status tp_cache8_workspace_size(const tp_dims* dims, const tp_cache8* cache, const tp_step* step, int64_t max_len,
+                                   size_t* bytes);
+
+/*
+ * Attention of a step's tokens over the cache, as tp_cache_attention: the same formulas, rows that attend to nothing, scores
+ * that count as infinities, workspace and errors.  A channel of a query that is 2^28 or more below its row's largest is
+ * taken to within 2^-39 of that one.  Every token of a sequence that has a page holds a key and a value (was loaded or
+ * appended); what lies behind the sequence's last token may be anything.
+ * Maxima, sums and outputs are held in fp32; the weights times the values' scales are rounded to fp16 (relative to the row's
+ * largest) for the value product.
+ */
+tp_status tp_cache8_attention(const tp_dims* dims, const tp_cache8* cache, const tp_step* step, const tp_rows* q,
+                              float softmax_scale, int64_t max_len, const tp_rows* o, float* lse, void* workspace,
+                              size_t ws_bytes, void* stream);
+
+/* Ranges of the sequences back as bf16 rows, as tp_cache_read: bf16(fp32(c * scale)) of the keys and values held. */
+tp_status tp_cache8_read(const tp_dims* dims, const tp_cache8* cache, const tp_batch* batch, const int64_t* first,
+                         void* k_out, void* v_out, void* stream);
 
 #ifdef __cplusplus
 }

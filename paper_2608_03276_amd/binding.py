@@ -28,7 +28,9 @@ EXPORTED = ("tp_version", "tp_status_string", "tp_last_error", "tp_keep_count", 
             "tp_combine_select_topk",
             "tp_combine_select_topk_static", "tp_compact_kv", "tp_compact_quantize_kv", "tp_evict",
             "tp_cache_page_bytes", "tp_cache_load", "tp_cache_append", "tp_cache_workspace_size",
-            "tp_cache_attention", "tp_cache_read")
+            "tp_cache_attention", "tp_cache_read",
+            "tp_cache8_page_bytes", "tp_cache8_load", "tp_cache8_append", "tp_cache8_workspace_size",
+            "tp_cache8_attention", "tp_cache8_read")
 TP_STATIC_SCRATCH_BYTES = 64 << 20
 TP_ROPE_HALVES, TP_ROPE_PAIRS = 0, 1
 
@@ -61,6 +63,10 @@ class TpCache(ctypes.Structure):
     _fields_ = [("pages", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
                 ("num_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("batch", ctypes.c_int32)]
+
+
+class TpCache8(ctypes.Structure):
+    _fields_ = [("cache", TpCache), ("qfmt", ctypes.c_int32)]
 
 
 class TpStep(ctypes.Structure):
@@ -172,6 +178,19 @@ def load():
     lib.tp_cache_attention.argtypes = [pd, pc, ps, pr, ctypes.c_float, ctypes.c_int64, pr, P, P, ctypes.c_size_t, P]
     lib.tp_cache_read.restype = ctypes.c_int32
     lib.tp_cache_read.argtypes = [pd, pc, pb, pi64, P, P, P]
+    pc8 = ctypes.POINTER(TpCache8)
+    lib.tp_cache8_page_bytes.restype = ctypes.c_size_t
+    lib.tp_cache8_page_bytes.argtypes = [pd, ctypes.c_int32]
+    lib.tp_cache8_load.restype = ctypes.c_int32
+    lib.tp_cache8_load.argtypes = [pd, pc8, pi64, P, P, P, ctypes.c_int32, P]
+    lib.tp_cache8_append.restype = ctypes.c_int32
+    lib.tp_cache8_append.argtypes = [pd, pc8, ps, pr, pr, P, ctypes.POINTER(TpRope), pr, pr, P]
+    lib.tp_cache8_workspace_size.restype = ctypes.c_int32
+    lib.tp_cache8_workspace_size.argtypes = [pd, pc8, ps, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)]
+    lib.tp_cache8_attention.restype = ctypes.c_int32
+    lib.tp_cache8_attention.argtypes = [pd, pc8, ps, pr, ctypes.c_float, ctypes.c_int64, pr, P, P, ctypes.c_size_t, P]
+    lib.tp_cache8_read.restype = ctypes.c_int32
+    lib.tp_cache8_read.argtypes = [pd, pc8, pb, pi64, P, P, P]
     _lib = lib
     return lib
 
@@ -507,8 +526,10 @@ class Cache:
     `lens` int32 [batch] (None for a cache that is only loaded).  All calls on one handle see what the
     tensors hold when the work runs, so lengths and table are updated in place from step to step."""
 
+    bits = 4  # of a code
+
     def __init__(self, d: TpDims, pages, page_table, lens, page_tokens: int):
-        each = tp_cache_page_bytes(d, page_tokens) * d.num_layers * d.num_kv_heads
+        each = self._page_bytes(d, page_tokens) * d.num_layers * d.num_kv_heads
         if not pages.is_cuda or not pages.is_contiguous():
             raise ValueError("pages must be a contiguous device tensor")
         if page_table.dim() != 2:
@@ -526,6 +547,29 @@ class Cache:
         self.c = TpCache(pages.data_ptr(), page_table.data_ptr(), None if lens is None else lens.data_ptr(),
                          _nbytes(pages) // each, int(page_tokens), page_table.shape[1], page_table.shape[0])
         self.ref = ctypes.byref(self.c)
+
+    @staticmethod
+    def _page_bytes(d: TpDims, page_tokens: int) -> int:
+        return tp_cache_page_bytes(d, page_tokens)
+
+
+class Cache8(Cache):
+    """A tp_cache8 and the tensors it points to: a Cache whose pages (tp_cache8_page_bytes) hold 8-bit codes of the
+    format `qfmt`, TP_QFMT_INT or TP_QFMT_FP8_E4M3."""
+
+    bits = 8
+
+    def __init__(self, d: TpDims, pages, page_table, lens, page_tokens: int, qfmt: int = TP_QFMT_INT):
+        super().__init__(d, pages, page_table, lens, page_tokens)
+        if qfmt not in (TP_QFMT_INT, TP_QFMT_FP8_E4M3):
+            raise ValueError(f"unknown qfmt {qfmt}")
+        self.qfmt = int(qfmt)
+        self.c = TpCache8(self.c, self.qfmt)
+        self.ref = ctypes.byref(self.c)
+
+    @staticmethod
+    def _page_bytes(d: TpDims, page_tokens: int) -> int:
+        return tp_cache8_page_bytes(d, page_tokens)
 
 
 class Step:
@@ -568,9 +612,15 @@ def _rows(t, layers: int, total: int, heads: int, head_dim: int, name: str):
                      f"{(layers, total, heads, head_dim)} ([L][total][heads][d]), the last dimension contiguous")
 
 
-def _cache_call(d: TpDims, cache: Cache, tensors, stream):
+def _cache8_call(d: TpDims, cache: Cache8, tensors, stream):
+    return _cache_call(d, cache, tensors, stream, 8)
+
+
+def _cache_call(d: TpDims, cache: Cache, tensors, stream, bits: int = 4):
     """The stream of a call (the current one of the cache's device), after the checks all calls share.  Kept lean: a
     decode step makes these calls for every layer."""
+    if cache.bits != bits:
+        raise ValueError(f"a cache of {cache.bits}-bit codes for a call on {bits}-bit ones")
     if bytes(d) != cache.dims:
         raise ValueError("the cache was made for other dims")
     index = cache.index
@@ -595,32 +645,27 @@ def _need_step(cache: Cache, step: Step):
         raise ValueError(f"offsets holds {step.batch + 1} entries, needs {cache.batch + 1}")
 
 
-def tp_cache_page_bytes(d: TpDims, page_tokens: int) -> int:
-    n = int(load().tp_cache_page_bytes(ctypes.byref(d), int(page_tokens)))
+def _page_bytes(call, d: TpDims, page_tokens: int) -> int:
+    n = int(call(ctypes.byref(d), int(page_tokens)))
     if n == 0:
         raise TaskPressError(TP_ERR_UNSUPPORTED, load().tp_last_error().decode())
     return n
 
 
-def tp_cache_load(d: TpDims, cache: Cache, kept_offsets, k, v_q, scales, bits: int, stream=None):
-    """The compact cache (k bf16 [L][Hkv][K_tot][d], v_q [L][Hkv][K_tot][d / 2], scales [L][Hkv][K_tot])
-    into the pages, as the first tokens of the cache's sequences."""
-    s = _cache_call(d, cache, (k, v_q, scales), stream)
+def _load(stream_of, call, row: int, d: TpDims, cache: Cache, kept_offsets, k, v_q, scales, bits: int, stream):
+    s = stream_of(d, cache, (k, v_q, scales), stream)
     n = d.num_layers * d.num_kv_heads * int(kept_offsets[-1])
     if len(kept_offsets) != cache.batch + 1:
         raise ValueError(f"kept_offsets holds {len(kept_offsets)} entries, needs {cache.batch + 1}")
     _need(k, n * d.head_dim * 2, "k")
-    _need(v_q, n * d.head_dim // 2, "v_q")
+    _need(v_q, n * row, "v_q")
     _need(scales, n * 4, "scales")
-    _on_device(cache, load().tp_cache_load, ctypes.byref(d), cache.ref, _i64_array(kept_offsets), _ptr(k), _ptr(v_q),
-               _ptr(scales), int(bits), s)
+    _on_device(cache, call, ctypes.byref(d), cache.ref, _i64_array(kept_offsets), _ptr(k), _ptr(v_q), _ptr(scales),
+               int(bits), s)
 
 
-def tp_cache_append(d: TpDims, cache: Cache, step: Step, k, v, positions=None, rope: Rope = None, q=None, q_out=None,
-                    stream=None):
-    """A step's keys (rotated at `positions` int32 [total]) and values into the pages, and q's rows rotated
-    into q_out.  k, v [total][Hkv][d], q, q_out [total][Hq][d] (or with a leading [L]), any strides."""
-    s = _cache_call(d, cache, (k, v, positions, q, q_out, step.offsets, None if rope is None else rope.cos_sin), stream)
+def _append(stream_of, call, d: TpDims, cache: Cache, step: Step, k, v, positions, rope, q, q_out, stream):
+    s = stream_of(d, cache, (k, v, positions, q, q_out, step.offsets, None if rope is None else rope.cos_sin), stream)
     _need_step(cache, step)
     L, Hq, Hkv, D, n = d.num_layers, d.num_q_heads, d.num_kv_heads, d.head_dim, step.total
     byref = ctypes.byref
@@ -628,8 +673,50 @@ def tp_cache_append(d: TpDims, cache: Cache, step: Step, k, v, positions=None, r
     ro = None if q_out is None else byref(_rows(q_out, L, n, Hq, D, "q_out"))
     if positions is not None:
         _device_tensor(positions, torch.int32, "positions", (n,))
-    _on_device(cache, load().tp_cache_append, byref(d), cache.ref, step.ref, byref(_rows(k, L, n, Hkv, D, "k")),
+    _on_device(cache, call, byref(d), cache.ref, step.ref, byref(_rows(k, L, n, Hkv, D, "k")),
                byref(_rows(v, L, n, Hkv, D, "v")), _ptr(positions), None if rope is None else rope.ref, rq, ro, s)
+
+
+def _attention(stream_of, call, size_of, d: TpDims, cache: Cache, step: Step, q, softmax_scale: float, max_len: int, o, lse,
+               workspace, stream):
+    s = stream_of(d, cache, (q, o, lse, workspace, step.offsets), stream)
+    _need_step(cache, step)
+    L, Hq, D, n = d.num_layers, d.num_q_heads, d.head_dim, step.total
+    byref = ctypes.byref
+    if lse is not None:
+        _need(lse, L * Hq * n * 4, "lse")
+    if workspace is None:
+        workspace = _workspace(size_of(d, cache, step, max_len), cache.device, stream)
+    _on_device(cache, call, byref(d), cache.ref, step.ref, byref(_rows(q, L, n, Hq, D, "q")), softmax_scale, max_len,
+               byref(_rows(o, L, n, Hq, D, "o")), _ptr(lse), workspace.data_ptr(), _nbytes(workspace), s)
+
+
+def _read(stream_of, call, d: TpDims, cache: Cache, batch: Batch, k_out, v_out, first, stream):
+    s = stream_of(d, cache, (k_out, v_out), stream)
+    n = d.num_layers * d.num_kv_heads * batch.n_tot * d.head_dim * 2
+    _need(k_out, n, "k_out")
+    _need(v_out, n, "v_out")
+    if first is not None and len(first) != cache.batch:
+        raise ValueError(f"first holds {len(first)} entries, needs {cache.batch}")
+    _on_device(cache, call, ctypes.byref(d), cache.ref, ctypes.byref(batch.c), None if first is None else _i64_array(first),
+               _ptr(k_out), _ptr(v_out), s)
+
+
+def tp_cache_page_bytes(d: TpDims, page_tokens: int) -> int:
+    return _page_bytes(load().tp_cache_page_bytes, d, page_tokens)
+
+
+def tp_cache_load(d: TpDims, cache: Cache, kept_offsets, k, v_q, scales, bits: int, stream=None):
+    """The compact cache (k bf16 [L][Hkv][K_tot][d], v_q [L][Hkv][K_tot][d / 2], scales [L][Hkv][K_tot])
+    into the pages, as the first tokens of the cache's sequences."""
+    _load(_cache_call, load().tp_cache_load, d.head_dim // 2, d, cache, kept_offsets, k, v_q, scales, bits, stream)
+
+
+def tp_cache_append(d: TpDims, cache: Cache, step: Step, k, v, positions=None, rope: Rope = None, q=None, q_out=None,
+                    stream=None):
+    """A step's keys (rotated at `positions` int32 [total]) and values into the pages, and q's rows rotated
+    into q_out.  k, v [total][Hkv][d], q, q_out [total][Hq][d] (or with a leading [L]), any strides."""
+    _append(_cache_call, load().tp_cache_append, d, cache, step, k, v, positions, rope, q, q_out, stream)
 
 
 def tp_cache_workspace_size(d: TpDims, cache: Cache, step: Step, max_len: int) -> int:
@@ -642,27 +729,47 @@ def tp_cache_attention(d: TpDims, cache: Cache, step: Step, q, softmax_scale: fl
                        workspace=None, stream=None):
     """Attention of a step's rows q [total][Hq][d] over the cache: o likewise (bf16), lse fp32 [L][Hq][total]
     (natural log) or None."""
-    s = _cache_call(d, cache, (q, o, lse, workspace, step.offsets), stream)
-    _need_step(cache, step)
-    L, Hq, D, n = d.num_layers, d.num_q_heads, d.head_dim, step.total
-    byref = ctypes.byref
-    if lse is not None:
-        _need(lse, L * Hq * n * 4, "lse")
-    if workspace is None:
-        workspace = _workspace(tp_cache_workspace_size(d, cache, step, max_len), cache.device, stream)
-    _on_device(cache, load().tp_cache_attention, byref(d), cache.ref, step.ref, byref(_rows(q, L, n, Hq, D, "q")),
-               softmax_scale, max_len, byref(_rows(o, L, n, Hq, D, "o")), _ptr(lse), workspace.data_ptr(),
-               _nbytes(workspace), s)
+    _attention(_cache_call, load().tp_cache_attention, tp_cache_workspace_size, d, cache, step, q, softmax_scale, max_len, o,
+               lse, workspace, stream)
 
 
 def tp_cache_read(d: TpDims, cache: Cache, batch: Batch, k_out, v_out, first=None, stream=None):
     """Tokens first[b] .. first[b] + n_b - 1 of each sequence (n_b from batch.ctx_offsets) as bf16 rows
     [L][Hkv][N_tot][d]."""
-    s = _cache_call(d, cache, (k_out, v_out), stream)
-    n = d.num_layers * d.num_kv_heads * batch.n_tot * d.head_dim * 2
-    _need(k_out, n, "k_out")
-    _need(v_out, n, "v_out")
-    if first is not None and len(first) != cache.batch:
-        raise ValueError(f"first holds {len(first)} entries, needs {cache.batch}")
-    _on_device(cache, load().tp_cache_read, ctypes.byref(d), cache.ref, ctypes.byref(batch.c),
-               None if first is None else _i64_array(first), _ptr(k_out), _ptr(v_out), s)
+    _read(_cache_call, load().tp_cache_read, d, cache, batch, k_out, v_out, first, stream)
+
+
+# ----------------------------------------------------------------------------- the paged 8-bit cache
+def tp_cache8_page_bytes(d: TpDims, page_tokens: int) -> int:
+    return _page_bytes(load().tp_cache8_page_bytes, d, page_tokens)
+
+
+def tp_cache8_load(d: TpDims, cache: Cache8, kept_offsets, k, v_q, scales, bits: int = 8, stream=None):
+    """The compact cache of an eviction in the cache's format into the pages, as tp_cache_load; bits: of the integer codes
+    v_q, whose rows are row_bytes(cache.qfmt, bits, d) long."""
+    _load(_cache8_call, load().tp_cache8_load, row_bytes(cache.qfmt, bits, d.head_dim) if cache.bits == 8 else 0, d, cache,
+          kept_offsets, k, v_q, scales, bits, stream)
+
+
+def tp_cache8_append(d: TpDims, cache: Cache8, step: Step, k, v, positions=None, rope: Rope = None, q=None, q_out=None,
+                     stream=None):
+    """A step's keys and values into the pages and its rotated queries into q_out, as tp_cache_append."""
+    _append(_cache8_call, load().tp_cache8_append, d, cache, step, k, v, positions, rope, q, q_out, stream)
+
+
+def tp_cache8_workspace_size(d: TpDims, cache: Cache8, step: Step, max_len: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().tp_cache8_workspace_size(ctypes.byref(d), cache.ref, step.ref, int(max_len), ctypes.byref(out)))
+    return int(out.value)
+
+
+def tp_cache8_attention(d: TpDims, cache: Cache8, step: Step, q, softmax_scale: float, max_len: int, o, lse=None,
+                        workspace=None, stream=None):
+    """Attention of a step's rows over the cache, as tp_cache_attention."""
+    _attention(_cache8_call, load().tp_cache8_attention, tp_cache8_workspace_size, d, cache, step, q, softmax_scale, max_len,
+               o, lse, workspace, stream)
+
+
+def tp_cache8_read(d: TpDims, cache: Cache8, batch: Batch, k_out, v_out, first=None, stream=None):
+    """Ranges of the sequences back as bf16 rows, as tp_cache_read."""
+    _read(_cache8_call, load().tp_cache8_read, d, cache, batch, k_out, v_out, first, stream)

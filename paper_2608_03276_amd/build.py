@@ -27,7 +27,7 @@ HIP_FLAGS = [
     "-I", os.path.join(ROOT, "include"),
 ]
 SOURCES = ["abi.cpp", "abi_cache.cpp", "guide_scores.hip", "guide_attention.hip", "quantize.hip", "select.hip", "compact.hip",
-           "cache_rows.hip", "cache_attention.hip"]
+           "cache_rows.hip", "cache_attention.hip", "abi_cache8.cpp", "cache8_rows.hip", "cache8_attention.hip"]
 # The score passes see finite inputs only (the ABI's precondition; -inf marks masked logits),
 # so max() need not quiet NaNs: this drops the canonicalising moves before every v_max.
 EXTRA_FLAGS = {"guide_scores.hip": ["-fno-honor-nans"]}

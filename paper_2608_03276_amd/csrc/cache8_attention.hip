@@ -1,0 +1,384 @@
+// Attention over the paged 8-bit cache (tp_cache8_attention): the newest tokens of each sequence, from one (decoding)
+// to a prompt's chunk, against all its tokens.
+//
+// The division of work is the 4-bit cache's (cache_attention.hip): a workgroup takes 16 to 64 query rows of one
+// (sequence, KV head) and one chunk of the context; its four or eight waves take every fourth or eighth block of 32
+// tokens, with the softmax's running reference and sum in one pass, and join through LDS; chunks join in a second
+// kernel.  Both products are on v_mfma_f32_16x16x32_f16 with the cache as the A operand:
+//   scores  S^T = C Q^T of the keys' codes, exact in fp16 (integers up to 127; e4m3 numbers, the smallest 2^-9);
+//           the block's key scale goes into the factor that turns a sum into an exponent, one number a block;
+//   output  O^T += C^T P^T of the values' codes, with the values' scales multiplied into the weights P.
+// Codes become fp16 operands in registers: 0x6400 | u is 1024 + u for a byte u = c + 128 (one byte permutation makes
+// two of them, one packed addition takes 1152 off), and an e4m3 pair is one conversion instruction.
+#include <algorithm>
+
+#include "cache8_block.h"
+#include "cache_join.h"
+
+namespace tp {
+namespace {
+
+// Eight codes as fp16 numbers c; magic: 0x64646464.
+template <bool FP8>
+__device__ inline Frag codes8(uint32_t lo, uint32_t hi, uint32_t magic) {
+  Frag f;
+  if (FP8) {
+    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
+    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
+    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
+    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+  } else {
+    const f16x2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = __builtin_amdgcn_perm(magic, i < 2 ? lo : hi, (i & 1) ? 0x04030402u : 0x04010400u);
+      f.w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, two) + off);
+    }
+  }
+  return f;
+}
+
+// NR tiles of 16 rows, W waves.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave
+// it out).
+template <int D, bool FP8, int NR, int W, bool ONCE>
+__global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)) void k_cache8_attention(CacheAttnArgs a) {
+  using B = Cache8Block<D>;
+  constexpr int KS = D / 32;  // products of a score: channels in steps of 32
+  constexpr int ND = D / 16;  // output tiles: channels in steps of 16
+  constexpr int kStride = D + 4;
+  constexpr int kPolicy = ONCE ? 2 : 0;  // nontemporal
+  __shared__ float lds_o[W][16][kStride];
+  __shared__ float2 lds_stat[W][16 * NR];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int g = lane >> 4, n = lane & 15;
+  const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest);
+  const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
+  const int chunk = a.by_groups.div(rest), group = a.by_groups.mod(rest, chunk);
+  const int b = blockIdx.y;
+  // 64 of the chunk's pages from page0 on, one a lane
+  int page0 = (chunk * a.chunk / kCacheBlock) >> a.c.page_shift;
+  const int32_t* row_pages = a.c.table + (int64_t)b * a.c.max_pages;
+  const auto load_pages = [&] {
+    const uint32_t at = (uint32_t)(page0 + lane);
+    const int page = (int)at < a.c.max_pages ? *(const int32_t*)((const char*)row_pages + 4 * (uint64_t)at) : -1;
+    return page < a.c.num_pages ? page : -1;
+  };
+  int pages = load_pages();
+  const StepSeq q = step_sequence(a.c, a.s, b);
+  const RowGroup rg = row_group(a, q, group, 16 * NR);
+  if (rg.row0 >= rg.rows || (chunk > 0 && chunk * a.chunk >= rg.keys)) return;
+
+  // Queries as the products' B operand, each row brought near 2^14 by a power of two: in registers, or, for several
+  // tiles, in LDS, one copy for the waves.
+  constexpr bool kShared = NR > 1;
+  __shared__ u32x4 lds_q[kShared ? NR * KS * 64 : 1];
+  Frag qf[kShared ? 1 : NR][KS];
+  __shared__ int lds_shift[kShared ? 16 * NR : 1];  // the powers of two that the rows were multiplied by
+  int shift = 0;                                    // (one tile: the lane's row's)
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    if (kShared && r != wave) continue;  // a wave prepares one tile
+    const int row = rg.row0 + r * 16 + n;
+    const int t = a.R.div(row);
+    const bool in = row < rg.rows;
+    const uint16_t* p = a.q.data + layer * a.q.layer + (q.row + t) * a.q.token + (head * (int)a.R.d + a.R.mod(row, t)) * a.q.head;
+    uint4 x[KS];
+    uint32_t top = 0;  // the row's largest magnitude, as bf16 bits
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      x[s] = in ? *(const uint4*)(p + s * 32 + g * 8) : make_uint4(0, 0, 0, 0);
+      const uint32_t w[4] = {x[s].x, x[s].y, x[s].z, x[s].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+    }
+    top = row_max(top);
+    const bool finite = top < 0x7F80u;
+    const int e = 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(top << 16));  // the largest comes to [2^14, 2^15)
+    shift = e;
+    if (kShared && g == 0) lds_shift[r * 16 + n] = e;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const uint32_t w[4] = {x[s].x, x[s].y, x[s].z, x[s].w};
+      Frag f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f.w[i] = pack_h(__builtin_amdgcn_ldexpf(__uint_as_float(w[i] << 16), e),
+                        __builtin_amdgcn_ldexpf(__uint_as_float(w[i] & 0xFFFF0000u), e));
+        if (!finite) f.w[i] = 0x7E007E00u;  // every score of the row is NaN, also where a code is 0
+      }
+      if (!kShared)
+        qf[kShared ? 0 : r][s] = f;
+      else
+        lds_q[(r * KS + s) * 64 + lane] = (u32x4){f.w[0], f.w[1], f.w[2], f.w[3]};
+    }
+  }
+  if (kShared) __syncthreads();
+  const auto query = [&](int r, int s) {
+    if (!kShared) return qf[kShared ? 0 : r][s];
+    Frag f;
+    const u32x4 x = lds_q[(r * KS + s) * 64 + lane];
+    f.w[0] = x.x;
+    f.w[1] = x.y;
+    f.w[2] = x.z;
+    f.w[3] = x.w;
+    return f;
+  };
+
+  uint32_t magic = 0x64646464u;
+  asm("" : "+v"(magic));
+
+  f32x4 acc[NR][ND];
+  float m[NR], l[NR];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    m[r] = -kFar;
+    l[r] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < ND; ++x) acc[r][x] = (f32x4){0, 0, 0, 0};
+  }
+
+  const int key0 = chunk * a.chunk, key1 = min(rg.keys, key0 + a.chunk);
+  const int j0 = key0 / kCacheBlock + wave, j1 = (key1 + kCacheBlock - 1) / kCacheBlock;  // every W-th block
+  const int all_seen = rg.before + a.R.div(rg.row0) + 1;  // keys before this one are seen by every row of the group
+
+  // Block j's part of the lane, in registers: keys' bytes and scale, values' bytes and scales.
+  u32x4 kw[2][D / 64], vw[D / 32], vs[2];
+  uint32_t ks = 0;
+  const auto page_of = [&](int j) { return __builtin_amdgcn_readlane(pages, (j >> a.c.page_shift) - page0); };
+  const auto block_at = [&](int j) {
+    const int page = max(page_of(j), 0);  // a missing page: any
+    const int64_t at = (((int64_t)layer * a.c.num_pages + page) * a.c.Hkv + head) << a.c.page_shift;
+    uint8_t* blk = a.c.pages + (at + (j & ((1 << a.c.page_shift) - 1))) * B::kBytes;
+    return __builtin_amdgcn_make_buffer_rsrc(blk, 0, B::kBytes, 0x00020000);
+  };
+  const auto load_keys = [&](__amdgpu_buffer_rsrc_t blk) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+        kw[u][i] = __builtin_amdgcn_raw_buffer_load_b128(blk, lane * 16, B::kKeys + u * 16 * D + i * 1024, kPolicy);
+    ks = __builtin_amdgcn_raw_buffer_load_b32(blk, 0, B::kKeyScale, kPolicy);
+  };
+  const auto load_values = [&](__amdgpu_buffer_rsrc_t blk) {
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) vw[x] = __builtin_amdgcn_raw_buffer_load_b128(blk, lane * 16, B::kValues + x * 1024, kPolicy);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) vs[u] = __builtin_amdgcn_raw_buffer_load_b128(blk, g * 16, B::kValueScales + u * 64, kPolicy);
+  };
+  if (j0 < j1) {
+    const auto blk = block_at(j0);
+    load_keys(blk);
+    load_values(blk);
+  }
+  // the group's tiles: a decoding sequence beside a prompt's chunk has one, whose weights alone are formed
+  const int tiles = (rg.rows - rg.row0 + 15) / 16;
+  for (int j = j0; j < j1; j += W) {
+    const bool missing = page_of(j) < 0;
+    const bool masked = missing || (j + 1) * kCacheBlock > all_seen;
+    if (masked) {  // what no row sees may be anything, what one does not see must not spoil a sum
+      if (missing) ks = 0;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          vs[u][i] = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(vs[u][i]), 0.0f, -kNoMax));
+      if (FP8) {  // e4m3 has NaN: bytes of tokens behind the last seen one are zeros
+        uint32_t keep[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int first = j * kCacheBlock + u * 16 + g * 4, count = missing ? 0 : min(max(rg.keys - first, 0), 4);
+          keep[u] = count == 4 ? 0xFFFFFFFFu : (1u << (8 * count)) - 1u;
+        }
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vw[x][i] &= keep[i & 1];
+      }
+    }
+    f32x4 xs[2][NR];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const u32x4 w = kw[u][s >> 1];
+        const Frag k = codes8<FP8>((s & 1) ? w.z : w.x, (s & 1) ? w.w : w.y, magic);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, query(r, s), xs[u][r]);
+      }
+    }
+    // softmax_scale * log2(e) * the keys' scale, as a number near softmax_scale's and a power of two
+    const float factor1 = a.scale_log2 * __builtin_amdgcn_frexp_mantf(__uint_as_float(ks));
+    const int power = __builtin_amdgcn_frexp_expf(__uint_as_float(ks));
+    // (after the last block, that block once more: no branch, so the registers stay in place)
+    const int jn = j + W < j1 ? j + W : j;
+    if ((jn >> a.c.page_shift) - page0 >= 64) {
+      page0 = jn >> a.c.page_shift;
+      pages = load_pages();
+    }
+    const auto next = block_at(jn);
+    __builtin_amdgcn_sched_barrier(0);
+    load_keys(next);
+
+    Frag pf[NR] = {};
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      if (r > 0 && r >= tiles) break;
+      float w[8], p[8], sum, top;
+      // above 0 and finite, so that an unseen token's -infinity and a score of 0 stay that
+      const float factor = __builtin_amdgcn_fmed3f(
+          __builtin_amdgcn_ldexpf(factor1, power - (kShared ? lds_shift[r * 16 + n] : shift)), 0x1p-149f, -kNoMax);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = __uint_as_float(vs[i >> 2][i & 3]);
+      if (masked) {
+        const int row = rg.row0 + r * 16 + n;
+        const int seen = missing || row >= rg.rows ? 0 : rg.before + a.R.div(row) + 1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (j * kCacheBlock + (i >> 2) * 16 + g * 4 + (i & 3) >= seen) xs[i >> 2][r][i & 3] = -INFINITY;
+      }
+      const auto weigh = [&] {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(fmaf(xs[i >> 2][r][i & 3], factor, -m[r]));
+          sum = i == 0 ? p[i] : sum + p[i];
+          p[i] *= w[i];
+          top = i == 0 ? p[i] : fmaxf(top, p[i]);
+        }
+      };
+      weigh();
+      if (__builtin_amdgcn_ballot_w64(fmaxf(top, sum * kLeastScale) > kLimit) != 0) {
+        float next = kNoMax;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          next = fmaxf(next, fmaf(xs[i >> 2][r][i & 3], factor, __builtin_amdgcn_logf(fmaxf(w[i], kLeastScale)) - kSet));
+        }
+        next = fmaxf(row_max(next), m[r]);
+        const float f = __builtin_amdgcn_exp2f(m[r] - next);
+        m[r] = next;
+        l[r] *= f;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) acc[r][i] *= f;
+        weigh();
+      }
+      l[r] += sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pf[r].w[i] = pack_h(p[2 * i], p[2 * i + 1]);
+    }
+#pragma unroll
+    for (int x = 0; x < ND; ++x) {
+      const u32x4 w = vw[x >> 1];
+      const Frag v = codes8<FP8>((x & 1) ? w.z : w.x, (x & 1) ? w.w : w.y, magic);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) acc[r][x] = mfma(v, pf[r], acc[r][x]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_values(next);
+  }
+
+  // join the waves
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    l[r] = row_sum(l[r]);
+    if (g == 0) lds_stat[wave][r * 16 + n] = make_float2(m[r], l[r]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    if (r > 0 && r >= tiles) break;
+    float top = kNoMax;
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, lds_stat[w][r * 16 + n].x);
+    const float f = __builtin_amdgcn_exp2f(m[r] - top);
+    if (r > 0) __syncthreads();
+#pragma unroll
+    for (int x = 0; x < ND; ++x) {
+      const f32x4 o = acc[r][x] * f;
+      *(f32x4*)&lds_o[wave][n][x * 16 + g * 4] = o;
+    }
+    __syncthreads();
+    // a row's channels by 4 W threads
+    constexpr int CH = D / (4 * W);
+    const int row16 = threadIdx.x / (4 * W), c0 = (threadIdx.x % (4 * W)) * CH;
+    const int row = rg.row0 + r * 16 + row16;
+    if (row < rg.rows) {
+      float2 st = make_float2(kNoMax, 0.0f);
+#pragma unroll
+      for (int w = 0; w < W; ++w) st.x = fmaxf(st.x, lds_stat[w][r * 16 + row16].x);
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float2 s = lds_stat[w][r * 16 + row16];
+        st.y += s.y * __builtin_amdgcn_exp2f(s.x - st.x);
+      }
+      float o[CH];
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        o[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) o[i] += lds_o[w][row16][c0 + i];
+      }
+      const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
+      const int64_t token = q.row + t;
+      if (rg.keys <= a.chunk) {  // the only chunk
+        store_output<CH>(a, layer, token, hq, c0, o, st);
+      } else {
+        const int64_t at = partial_row(a, chunk, b, lh, row);
+        if (c0 == 0) a.stat[at] = st;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) a.part[at * D + c0 + i] = o[i];
+      }
+    }
+  }
+}
+
+}  // namespace
+
+constexpr int64_t kStreamed = 256 << 20;  // bytes of a cache that the chip's caches do not hold
+
+// The 4-bit cache's division into rows and chunks, with this cache's bytes.
+CachePlan cache8_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
+                      int32_t max_len) {
+  CachePlan p = cache_plan(L, Hq, Hkv, head_dim, batch, max_new, max_len);
+  p.once = p.row_groups == 1 && (double)L * Hkv * batch * max_len * (double)cache8_block_bytes(head_dim) / kCacheBlock >
+                                    (double)kStreamed;
+  return p;
+}
+
+namespace {
+
+template <int D, bool FP8, int NR, int W>
+void launch_part(const CacheAttnArgs& a, dim3 grid, hipStream_t stream) {
+  if (a.once)
+    hipLaunchKernelGGL((k_cache8_attention<D, FP8, NR, W, true>), grid, dim3(64 * W), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_cache8_attention<D, FP8, NR, W, false>), grid, dim3(64 * W), 0, stream, a);
+}
+
+template <int D, bool FP8>
+hipError_t launch_attention(const CacheAttnArgs& a, hipStream_t stream) {
+  const unsigned heads = (unsigned)(a.c.L * a.c.Hkv), batch = (unsigned)a.c.batch;
+  const dim3 grid(heads * a.row_groups * a.chunks, batch);
+  if (a.tiles == 1 && a.waves == 8) launch_part<D, FP8, 1, 8>(a, grid, stream);
+  else if (a.tiles == 1) launch_part<D, FP8, 1, 4>(a, grid, stream);
+  else if (a.tiles == 2) launch_part<D, FP8, 2, 4>(a, grid, stream);
+  else launch_part<D, FP8, 4, 4>(a, grid, stream);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.chunks == 1) return e;
+  const unsigned rows = heads * a.row_groups * a.tiles * 16;  // 16 a tile
+  if (a.chunks >= 8)
+    hipLaunchKernelGGL((k_cache_merge<D, 4>), dim3(rows, batch), dim3(kMergeThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_cache_merge<D, 1>), dim3(rows / 4, batch), dim3(kMergeThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache8_attention(const CacheAttnArgs& a, bool fp8, int head_dim, hipStream_t stream) {
+  if (head_dim == 128) return fp8 ? launch_attention<128, true>(a, stream) : launch_attention<128, false>(a, stream);
+  return fp8 ? launch_attention<64, true>(a, stream) : launch_attention<64, false>(a, stream);
+}
+
+}  // namespace tp
