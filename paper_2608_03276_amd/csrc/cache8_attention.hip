@@ -38,6 +38,28 @@ __device__ inline Frag codes8(uint32_t lo, uint32_t hi, uint32_t magic) {
   return f;
 }
 
+// Copies straight into LDS, 16 or 4 bytes a lane: lane i's land at lds + 16 i (4 i).  In assembly, because the compiler
+// would wait for all of them before every LDS read that follows; the kernel waits for those that it needs.
+template <bool ONCE>
+__device__ inline void copy16(uint32_t offset, const uint8_t* from, uint32_t lds) {
+  if (ONCE)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(offset), "s"(from), "s"(lds) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(lds) : "memory", "m0");
+}
+template <bool ONCE>
+__device__ inline void copy4(uint32_t offset, const uint8_t* from, uint32_t lds) {
+  if (ONCE)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1 nt" ::"v"(offset), "s"(from), "s"(lds) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(from), "s"(lds) : "memory", "m0");
+}
+template <int N>
+__device__ inline void wait_copies_but() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ inline void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // NR tiles of 16 rows, W waves.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave
 // it out).
 template <int D, bool FP8, int NR, int W, bool ONCE>
@@ -47,8 +69,14 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
   constexpr int ND = D / 16;  // output tiles: channels in steps of 16
   constexpr int kStride = D + 4;
   constexpr int kPolicy = ONCE ? 2 : 0;  // nontemporal
-  __shared__ float lds_o[W][16][kStride];
+  // Four tiles leave no registers for a block ahead: it waits in LDS, the wave's own keys and, twice, values and scales.
+  constexpr bool kStaged = NR == 4;
+  constexpr int kCodes = 32 * D, kScales = 256, kWaveStage = kStaged ? 3 * kCodes + 2 * kScales : 0;
+  constexpr int kJoin = 16 * kStride * 4;  // bytes of a wave's outputs of a tile
+  constexpr int kWaveLds = kWaveStage > kJoin ? kWaveStage : kJoin;
+  __shared__ alignas(16) uint8_t lds_wave[W * kWaveLds];
   __shared__ float2 lds_stat[W][16 * NR];
+  const auto lds_o = [&](int w, int row, int x) { return (float*)(lds_wave + w * kWaveLds) + row * kStride + x; };
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15;
@@ -142,40 +170,90 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
   const int j0 = key0 / kCacheBlock + wave, j1 = (key1 + kCacheBlock - 1) / kCacheBlock;  // every W-th block
   const int all_seen = rg.before + a.R.div(rg.row0) + 1;  // keys before this one are seen by every row of the group
 
-  // Block j's part of the lane, in registers: keys' bytes and scale, values' bytes and scales.
+  // Block j's part of the lane: keys' bytes and scale, values' bytes and scales, in registers or in LDS.
   u32x4 kw[2][D / 64], vw[D / 32], vs[2];
   uint32_t ks = 0;
+  uint8_t* const stage = lds_wave + wave * kWaveLds;
+  const uint32_t stage_at = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stage);
+  constexpr int kCopies = D / 32 + 1;  // of a block's values and scales (its keys': D / 32)
+  int half = 0;                        // the block's values are in the first or second half of theirs
   const auto page_of = [&](int j) { return __builtin_amdgcn_readlane(pages, (j >> a.c.page_shift) - page0); };
   const auto block_at = [&](int j) {
     const int page = max(page_of(j), 0);  // a missing page: any
     const int64_t at = (((int64_t)layer * a.c.num_pages + page) * a.c.Hkv + head) << a.c.page_shift;
-    uint8_t* blk = a.c.pages + (at + (j & ((1 << a.c.page_shift) - 1))) * B::kBytes;
-    return __builtin_amdgcn_make_buffer_rsrc(blk, 0, B::kBytes, 0x00020000);
+    return a.c.pages + (at + (j & ((1 << a.c.page_shift) - 1))) * B::kBytes;
   };
-  const auto load_keys = [&](__amdgpu_buffer_rsrc_t blk) {
+  const auto buffer = [&](uint8_t* blk) { return __builtin_amdgcn_make_buffer_rsrc(blk, 0, B::kBytes, 0x00020000); };
+  const auto load_keys = [&](uint8_t* blk) {
+    if (kStaged) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) copy16<ONCE>(lane * 16, blk + B::kKeys + i * 1024, stage_at + i * 1024);
+      return;
+    }
+    const auto r = buffer(blk);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < D / 64; ++i)
-        kw[u][i] = __builtin_amdgcn_raw_buffer_load_b128(blk, lane * 16, B::kKeys + u * 16 * D + i * 1024, kPolicy);
-    ks = __builtin_amdgcn_raw_buffer_load_b32(blk, 0, B::kKeyScale, kPolicy);
+        kw[u][i] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, B::kKeys + u * 16 * D + i * 1024, kPolicy);
+    ks = __builtin_amdgcn_raw_buffer_load_b32(r, 0, B::kKeyScale, kPolicy);
   };
-  const auto load_values = [&](__amdgpu_buffer_rsrc_t blk) {
+  const auto load_values = [&](uint8_t* blk, int to) {
+    if (kStaged) {
+      const uint32_t at = stage_at + kCodes + to * (kCodes + kScales);
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x) vw[x] = __builtin_amdgcn_raw_buffer_load_b128(blk, lane * 16, B::kValues + x * 1024, kPolicy);
+      for (int i = 0; i < D / 32; ++i) copy16<ONCE>(lane * 16, blk + B::kValues + i * 1024, at + i * 1024);
+      copy4<ONCE>(min(lane, 32) * 4, blk + B::kValueScales, at + kCodes);  // the values', then the keys'
+      return;
+    }
+    const auto r = buffer(blk);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) vs[u] = __builtin_amdgcn_raw_buffer_load_b128(blk, g * 16, B::kValueScales + u * 64, kPolicy);
+    for (int x = 0; x < D / 32; ++x) vw[x] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, B::kValues + x * 1024, kPolicy);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) vs[u] = __builtin_amdgcn_raw_buffer_load_b128(r, g * 16, B::kValueScales + u * 64, kPolicy);
   };
   if (j0 < j1) {
-    const auto blk = block_at(j0);
+    uint8_t* blk = block_at(j0);
     load_keys(blk);
-    load_values(blk);
+    load_values(blk, 0);
   }
   // the group's tiles: a decoding sequence beside a prompt's chunk has one, whose weights alone are formed
   const int tiles = (rg.rows - rg.row0 + 15) / 16;
   for (int j = j0; j < j1; j += W) {
     const bool missing = page_of(j) < 0;
     const bool masked = missing || (j + 1) * kCacheBlock > all_seen;
+    uint8_t* const values = stage + kCodes + half * (kCodes + kScales);
+    if (kStaged) wait_copies_but<kCopies>();  // the keys are there
+    f32x4 xs[2][NR];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        if (kStaged && (s & 1) == 0) kw[u][s >> 1] = *(const u32x4*)(stage + u * 16 * D + (s >> 1) * 1024 + lane * 16);
+        const u32x4 w = kw[u][s >> 1];
+        const Frag k = codes8<FP8>((s & 1) ? w.z : w.x, (s & 1) ? w.w : w.y, magic);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, query(r, s), xs[u][r]);
+      }
+    }
+    // (after the last block, that block once more: no branch, so the registers stay in place)
+    const int jn = j + W < j1 ? j + W : j;
+    if ((jn >> a.c.page_shift) - page0 >= 64) {
+      page0 = jn >> a.c.page_shift;
+      pages = load_pages();
+    }
+    uint8_t* const next = block_at(jn);
+    __builtin_amdgcn_sched_barrier(0);
+    if (kStaged) {
+      wait_lds_reads();
+      load_keys(next);
+      wait_copies_but<D / 32>();  // the values and scales are there
+#pragma unroll
+      for (int u = 0; u < 2; ++u) vs[u] = *(const u32x4*)(values + kCodes + u * 64 + g * 16);
+      ks = *(const uint32_t*)(values + kCodes + 128);
+    }
     if (masked) {  // what no row sees may be anything, what one does not see must not spoil a sum
       if (missing) ks = 0;
 #pragma unroll
@@ -191,36 +269,18 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
           keep[u] = count == 4 ? 0xFFFFFFFFu : (1u << (8 * count)) - 1u;
         }
 #pragma unroll
-        for (int x = 0; x < D / 32; ++x)
+        for (int x = 0; x < D / 32; ++x) {
+          if (kStaged) vw[x] = *(const u32x4*)(values + x * 1024 + lane * 16);
 #pragma unroll
           for (int i = 0; i < 4; ++i) vw[x][i] &= keep[i & 1];
-      }
-    }
-    f32x4 xs[2][NR];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const u32x4 w = kw[u][s >> 1];
-        const Frag k = codes8<FP8>((s & 1) ? w.z : w.x, (s & 1) ? w.w : w.y, magic);
-#pragma unroll
-        for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, query(r, s), xs[u][r]);
+          if (kStaged) *(u32x4*)(values + x * 1024 + lane * 16) = vw[x];
+        }
       }
     }
     // softmax_scale * log2(e) * the keys' scale, as a number near softmax_scale's and a power of two
     const float factor1 = a.scale_log2 * __builtin_amdgcn_frexp_mantf(__uint_as_float(ks));
     const int power = __builtin_amdgcn_frexp_expf(__uint_as_float(ks));
-    // (after the last block, that block once more: no branch, so the registers stay in place)
-    const int jn = j + W < j1 ? j + W : j;
-    if ((jn >> a.c.page_shift) - page0 >= 64) {
-      page0 = jn >> a.c.page_shift;
-      pages = load_pages();
-    }
-    const auto next = block_at(jn);
-    __builtin_amdgcn_sched_barrier(0);
-    load_keys(next);
+    if (!kStaged) load_keys(next);  // (the keys' scale is used)
 
     Frag pf[NR] = {};
 #pragma unroll
@@ -269,14 +329,17 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
     }
 #pragma unroll
     for (int x = 0; x < ND; ++x) {
+      if (kStaged && (x & 1) == 0) vw[x >> 1] = *(const u32x4*)(values + (x >> 1) * 1024 + lane * 16);
       const u32x4 w = vw[x >> 1];
       const Frag v = codes8<FP8>((x & 1) ? w.z : w.x, (x & 1) ? w.w : w.y, magic);
 #pragma unroll
       for (int r = 0; r < NR; ++r) acc[r][x] = mfma(v, pf[r], acc[r][x]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    load_values(next);
+    half ^= kStaged ? 1 : 0;
+    load_values(next, half);
   }
+  if (kStaged) wait_copies_but<0>();  // the last ones land before the outputs take their place
 
   // join the waves
 #pragma unroll
@@ -296,7 +359,7 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
 #pragma unroll
     for (int x = 0; x < ND; ++x) {
       const f32x4 o = acc[r][x] * f;
-      *(f32x4*)&lds_o[wave][n][x * 16 + g * 4] = o;
+      *(f32x4*)lds_o(wave, n, x * 16 + g * 4) = o;
     }
     __syncthreads();
     // a row's channels by 4 W threads
@@ -317,7 +380,7 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
       for (int i = 0; i < CH; ++i) {
         o[i] = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) o[i] += lds_o[w][row16][c0 + i];
+        for (int w = 0; w < W; ++w) o[i] += *lds_o(w, row16, c0 + i);
       }
       const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
       const int64_t token = q.row + t;
