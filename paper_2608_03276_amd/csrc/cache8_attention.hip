@@ -71,7 +71,7 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
   constexpr int kPolicy = ONCE ? 2 : 0;  // nontemporal
   // Four tiles leave no registers for a block ahead: it waits in LDS, the wave's own keys and, twice, values and scales.
   constexpr bool kStaged = NR == 4;
-  constexpr int kCodes = 32 * D, kScales = 256, kWaveStage = kStaged ? 3 * kCodes + 2 * kScales : 0;
+  constexpr int kCodes = 32 * D, kScales = 256, kWaveStage = kStaged ? 2 * kCodes + kScales : 0;
   constexpr int kJoin = 16 * kStride * 4;  // bytes of a wave's outputs of a tile
   constexpr int kWaveLds = kWaveStage > kJoin ? kWaveStage : kJoin;
   __shared__ alignas(16) uint8_t lds_wave[W * kWaveLds];
@@ -96,6 +96,87 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
   const StepSeq q = step_sequence(a.c, a.s, b);
   const RowGroup rg = row_group(a, q, group, 16 * NR);
   if (rg.row0 >= rg.rows || (chunk > 0 && chunk * a.chunk >= rg.keys)) return;
+
+  uint32_t magic = 0x64646464u;
+  asm("" : "+v"(magic));
+
+  const int key0 = chunk * a.chunk, key1 = min(rg.keys, key0 + a.chunk);
+  const int j0 = key0 / kCacheBlock + wave, j1 = (key1 + kCacheBlock - 1) / kCacheBlock;  // every W-th block
+  const int all_seen = rg.before + a.R.div(rg.row0) + 1;  // keys before this one are seen by every row of the group
+
+  // Block j's part of the lane: keys' bytes and scale, values' bytes and scales, in registers or in LDS.
+  u32x4 kw[2][D / 64], vw[D / 32], vs[2];
+  uint32_t ks = 0;
+  uint8_t* const stage = lds_wave + wave * kWaveLds;
+  const uint32_t stage_at = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stage);
+  constexpr int kCopies = D / 32;  // of a block's keys, and of its values
+  // Block j of the wave, in turn; whether it has no page (then it is that of any page).
+  const auto block_at = [&](int j, bool& missing) {
+    if ((j >> a.c.page_shift) - page0 >= 64) {
+      page0 = j >> a.c.page_shift;
+      pages = load_pages();
+    }
+    int page = __builtin_amdgcn_readlane(pages, (j >> a.c.page_shift) - page0);
+    missing = page < 0;
+    page = max(page, 0);
+    const int64_t at = (((int64_t)layer * a.c.num_pages + page) * a.c.Hkv + head) << a.c.page_shift;
+    return a.c.pages + (at + (j & ((1 << a.c.page_shift) - 1))) * B::kBytes;
+  };
+  const auto buffer = [&](uint8_t* blk) { return __builtin_amdgcn_make_buffer_rsrc(blk, 0, B::kBytes, 0x00020000); };
+  const auto load_keys = [&](uint8_t* blk) {
+    if (kStaged) {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) copy16<ONCE>(lane * 16, blk + B::kKeys + i * 1024, stage_at + i * 1024);
+      return;
+    }
+    const auto r = buffer(blk);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+        kw[u][i] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, B::kKeys + u * 16 * D + i * 1024, kPolicy);
+    ks = __builtin_amdgcn_raw_buffer_load_b32(r, 0, B::kKeyScale, kPolicy);
+  };
+  const auto load_values = [&](uint8_t* blk) {
+    if (kStaged) {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) copy16<ONCE>(lane * 16, blk + B::kValues + i * 1024, stage_at + kCodes + i * 1024);
+      copy4<ONCE>(min(lane, 32) * 4, blk + B::kValueScales, stage_at + 2 * kCodes);  // the values', then the keys'
+      return;
+    }
+    const auto r = buffer(blk);
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) vw[x] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, B::kValues + x * 1024, kPolicy);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) vs[u] = __builtin_amdgcn_raw_buffer_load_b128(r, g * 16, B::kValueScales + u * 64, kPolicy);
+  };
+  // What is staged, from LDS into registers.
+  const auto read_keys = [&] {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) kw[u][i] = *(const u32x4*)(stage + u * 16 * D + i * 1024 + lane * 16);
+  };
+  const auto read_values = [&] {
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) vw[x] = *(const u32x4*)(stage + kCodes + x * 1024 + lane * 16);
+  };
+  const auto key = [&](int u, int s) {
+    const u32x4 w = kw[u][s >> 1];
+    return codes8<FP8>((s & 1) ? w.z : w.x, (s & 1) ? w.w : w.y, magic);
+  };
+  const auto value = [&](int x) {
+    const u32x4 w = vw[x >> 1];
+    return codes8<FP8>((x & 1) ? w.z : w.x, (x & 1) ? w.w : w.y, magic);
+  };
+  bool missing = false, next_missing = false;
+  uint8_t* next = nullptr;
+  if (j0 < j1) {
+    next = block_at(j0, missing);
+    next_missing = missing;
+    load_keys(next);
+    load_values(next);
+  }
 
   // Queries as the products' B operand, each row brought near 2^14 by a power of two: in registers, or, for several
   // tiles, in LDS, one copy for the waves.
@@ -153,9 +234,6 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
     return f;
   };
 
-  uint32_t magic = 0x64646464u;
-  asm("" : "+v"(magic));
-
   f32x4 acc[NR][ND];
   float m[NR], l[NR];
 #pragma unroll
@@ -166,116 +244,75 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
     for (int x = 0; x < ND; ++x) acc[r][x] = (f32x4){0, 0, 0, 0};
   }
 
-  const int key0 = chunk * a.chunk, key1 = min(rg.keys, key0 + a.chunk);
-  const int j0 = key0 / kCacheBlock + wave, j1 = (key1 + kCacheBlock - 1) / kCacheBlock;  // every W-th block
-  const int all_seen = rg.before + a.R.div(rg.row0) + 1;  // keys before this one are seen by every row of the group
-
-  // Block j's part of the lane: keys' bytes and scale, values' bytes and scales, in registers or in LDS.
-  u32x4 kw[2][D / 64], vw[D / 32], vs[2];
-  uint32_t ks = 0;
-  uint8_t* const stage = lds_wave + wave * kWaveLds;
-  const uint32_t stage_at = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stage);
-  constexpr int kCopies = D / 32 + 1;  // of a block's values and scales (its keys': D / 32)
-  int half = 0;                        // the block's values are in the first or second half of theirs
-  const auto page_of = [&](int j) { return __builtin_amdgcn_readlane(pages, (j >> a.c.page_shift) - page0); };
-  const auto block_at = [&](int j) {
-    const int page = max(page_of(j), 0);  // a missing page: any
-    const int64_t at = (((int64_t)layer * a.c.num_pages + page) * a.c.Hkv + head) << a.c.page_shift;
-    return a.c.pages + (at + (j & ((1 << a.c.page_shift) - 1))) * B::kBytes;
-  };
-  const auto buffer = [&](uint8_t* blk) { return __builtin_amdgcn_make_buffer_rsrc(blk, 0, B::kBytes, 0x00020000); };
-  const auto load_keys = [&](uint8_t* blk) {
-    if (kStaged) {
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) copy16<ONCE>(lane * 16, blk + B::kKeys + i * 1024, stage_at + i * 1024);
-      return;
-    }
-    const auto r = buffer(blk);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i)
-        kw[u][i] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, B::kKeys + u * 16 * D + i * 1024, kPolicy);
-    ks = __builtin_amdgcn_raw_buffer_load_b32(r, 0, B::kKeyScale, kPolicy);
-  };
-  const auto load_values = [&](uint8_t* blk, int to) {
-    if (kStaged) {
-      const uint32_t at = stage_at + kCodes + to * (kCodes + kScales);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) copy16<ONCE>(lane * 16, blk + B::kValues + i * 1024, at + i * 1024);
-      copy4<ONCE>(min(lane, 32) * 4, blk + B::kValueScales, at + kCodes);  // the values', then the keys'
-      return;
-    }
-    const auto r = buffer(blk);
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x) vw[x] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, B::kValues + x * 1024, kPolicy);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) vs[u] = __builtin_amdgcn_raw_buffer_load_b128(r, g * 16, B::kValueScales + u * 64, kPolicy);
-  };
-  if (j0 < j1) {
-    uint8_t* blk = block_at(j0);
-    load_keys(blk);
-    load_values(blk, 0);
+  if (kStaged && j0 < j1) {
+    if (j0 + W < j1) next = block_at(j0 + W, next_missing);
+    wait_copies_but<kCopies + 1>();
+    read_keys();
+    wait_lds_reads();
+    load_keys(next);
   }
   // the group's tiles: a decoding sequence beside a prompt's chunk has one, whose weights alone are formed
   const int tiles = (rg.rows - rg.row0 + 15) / 16;
   for (int j = j0; j < j1; j += W) {
-    const bool missing = page_of(j) < 0;
     const bool masked = missing || (j + 1) * kCacheBlock > all_seen;
-    uint8_t* const values = stage + kCodes + half * (kCodes + kScales);
-    if (kStaged) wait_copies_but<kCopies>();  // the keys are there
     f32x4 xs[2][NR];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
+    if (kStaged) {
+      // Operands are read and formed a product ahead: the LDS's latency and the conversions pass beside the products.
+      Frag qn[NR], kn[2];
+#pragma unroll
+      for (int r = 0; r < NR; ++r) qn[r] = query(r, 0);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) kn[u] = key(u, 0);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        if (kStaged && (s & 1) == 0) kw[u][s >> 1] = *(const u32x4*)(stage + u * 16 * D + (s >> 1) * 1024 + lane * 16);
-        const u32x4 w = kw[u][s >> 1];
-        const Frag k = codes8<FP8>((s & 1) ? w.z : w.x, (s & 1) ? w.w : w.y, magic);
+        Frag q[NR], k[2];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, query(r, s), xs[u][r]);
+        for (int r = 0; r < NR; ++r) q[r] = qn[r];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) k[u] = kn[u];
+        if (s + 1 < KS) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) qn[r] = query(r, s + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (s + 1 < KS) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) kn[u] = key(u, s + 1);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k[u], q[r], xs[u][r]);
+        __builtin_amdgcn_sched_barrier(0);
       }
-    }
-    // (after the last block, that block once more: no branch, so the registers stay in place)
-    const int jn = j + W < j1 ? j + W : j;
-    if ((jn >> a.c.page_shift) - page0 >= 64) {
-      page0 = jn >> a.c.page_shift;
-      pages = load_pages();
-    }
-    uint8_t* const next = block_at(jn);
-    __builtin_amdgcn_sched_barrier(0);
-    if (kStaged) {
-      wait_lds_reads();
-      load_keys(next);
-      wait_copies_but<D / 32>();  // the values and scales are there
+      wait_copies_but<kCopies>();  // the values and scales are there
 #pragma unroll
-      for (int u = 0; u < 2; ++u) vs[u] = *(const u32x4*)(values + kCodes + u * 64 + g * 16);
-      ks = *(const uint32_t*)(values + kCodes + 128);
+      for (int u = 0; u < 2; ++u) vs[u] = *(const u32x4*)(stage + 2 * kCodes + u * 64 + g * 16);
+      ks = *(const uint32_t*)(stage + 2 * kCodes + 128);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const Frag k = key(u, s);
+#pragma unroll
+          for (int r = 0; r < NR; ++r) xs[u][r] = mfma(k, query(r, s), xs[u][r]);
+        }
+      // (after the last block, that block once more: no branch, so the registers stay in place)
+      next = block_at(j + W < j1 ? j + W : j, next_missing);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (masked) {  // what no row sees may be anything, what one does not see must not spoil a sum
+    if (masked) {  // scales that no row sees may be anything, those that one does not see must be finite
       if (missing) ks = 0;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           vs[u][i] = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(vs[u][i]), 0.0f, -kNoMax));
-      if (FP8) {  // e4m3 has NaN: bytes of tokens behind the last seen one are zeros
-        uint32_t keep[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int first = j * kCacheBlock + u * 16 + g * 4, count = missing ? 0 : min(max(rg.keys - first, 0), 4);
-          keep[u] = count == 4 ? 0xFFFFFFFFu : (1u << (8 * count)) - 1u;
-        }
-#pragma unroll
-        for (int x = 0; x < D / 32; ++x) {
-          if (kStaged) vw[x] = *(const u32x4*)(values + x * 1024 + lane * 16);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) vw[x][i] &= keep[i & 1];
-          if (kStaged) *(u32x4*)(values + x * 1024 + lane * 16) = vw[x];
-        }
-      }
     }
     // softmax_scale * log2(e) * the keys' scale, as a number near softmax_scale's and a power of two
     const float factor1 = a.scale_log2 * __builtin_amdgcn_frexp_mantf(__uint_as_float(ks));
@@ -294,10 +331,12 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
       for (int i = 0; i < 8; ++i) w[i] = __uint_as_float(vs[i >> 2][i & 3]);
       if (masked) {
         const int row = rg.row0 + r * 16 + n;
-        const int seen = missing || row >= rg.rows ? 0 : rg.before + a.R.div(row) + 1;
+        int seen = missing || row >= rg.rows ? 0 : rg.before + a.R.div(row) + 1;
+        seen -= j * kCacheBlock + g * 4;
+        asm volatile("" : "+v"(seen));
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (j * kCacheBlock + (i >> 2) * 16 + g * 4 + (i & 3) >= seen) xs[i >> 2][r][i & 3] = -INFINITY;
+          if ((i >> 2) * 16 + (i & 3) >= seen) xs[i >> 2][r][i & 3] = -INFINITY;
       }
       const auto weigh = [&] {
 #pragma unroll
@@ -309,11 +348,13 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
         }
       };
       weigh();
-      if (__builtin_amdgcn_ballot_w64(fmaxf(top, sum * kLeastScale) > kLimit) != 0) {
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(fmaxf(top, sum * kLeastScale) > kLimit) != 0, false)) {
         float next = kNoMax;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          next = fmaxf(next, fmaf(xs[i >> 2][r][i & 3], factor, __builtin_amdgcn_logf(fmaxf(w[i], kLeastScale)) - kSet));
+          float v = w[i];
+          asm volatile("" : "+v"(v));
+          next = fmaxf(next, fmaf(xs[i >> 2][r][i & 3], factor, __builtin_amdgcn_logf(fmaxf(v, kLeastScale)) - kSet));
         }
         next = fmaxf(row_max(next), m[r]);
         const float f = __builtin_amdgcn_exp2f(m[r] - next);
@@ -326,18 +367,45 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
       l[r] += sum;
 #pragma unroll
       for (int i = 0; i < 4; ++i) pf[r].w[i] = pack_h(p[2 * i], p[2 * i + 1]);
+      if (kStaged && r == 0) {
+        read_values();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (kStaged) {
+      wait_lds_reads();
+      load_values(next);
+      wait_copies_but<kCopies + 1>();  // the next block's keys are there
+      read_keys();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (FP8 && masked) {  // e4m3 has NaN: bytes of tokens behind the last seen one are zeros
+      uint32_t keep[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int first = j * kCacheBlock + u * 16 + g * 4, count = missing ? 0 : min(max(rg.keys - first, 0), 4);
+        keep[u] = count == 4 ? 0xFFFFFFFFu : (1u << (8 * count)) - 1u;
+      }
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vw[x][i] &= keep[i & 1];
     }
 #pragma unroll
     for (int x = 0; x < ND; ++x) {
-      if (kStaged && (x & 1) == 0) vw[x >> 1] = *(const u32x4*)(values + (x >> 1) * 1024 + lane * 16);
-      const u32x4 w = vw[x >> 1];
-      const Frag v = codes8<FP8>((x & 1) ? w.z : w.x, (x & 1) ? w.w : w.y, magic);
+      const Frag v = value(x);
 #pragma unroll
       for (int r = 0; r < NR; ++r) acc[r][x] = mfma(v, pf[r], acc[r][x]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    half ^= kStaged ? 1 : 0;
-    load_values(next, half);
+    missing = next_missing;
+    if (kStaged) {
+      if (j + 2 * W < j1) next = block_at(j + 2 * W, next_missing);
+      wait_lds_reads();
+      load_keys(next);
+    } else {
+      load_values(next);
+    }
   }
   if (kStaged) wait_copies_but<0>();  // the last ones land before the outputs take their place
 
