@@ -145,7 +145,7 @@ inline tp_status prepare_attention(decltype(&cache_plan) plan_of, const tp_dims*
   a.heads = Divisor::of((int64_t)dims->num_layers * dims->num_kv_heads);
   a.by_Hkv = Divisor::of(dims->num_kv_heads);
   a.by_groups = Divisor::of(plan.row_groups);
-  a.by_chunk = Divisor::of(plan.chunk);
+  a.by_chunk = Divisor::of(std::max(plan.chunk, 1));
   a.tiles = plan.tiles;
   a.row_groups = plan.row_groups;
   a.chunk = plan.chunk;

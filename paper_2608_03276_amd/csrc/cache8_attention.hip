@@ -60,16 +60,104 @@ __device__ inline void wait_copies_but() {
 }
 __device__ inline void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// NR tiles of 16 rows, W waves.  ONCE: the cache is read once and is not found in a cache by the next call (loads leave
-// it out).
+// Division of a decoding call's work on the device, where the lengths are known: the (sequence, head) pairs in a row
+// (sequences, then heads), each as long as its blocks and what starting on it costs, are cut into equal shares, one a
+// workgroup.  A share holds several short pairs or a part of a long one; a pair whose blocks lie in several shares has a
+// partial result in each, which k_cache8_join_shares joins.  So what a call costs goes by what its sequences hold and not
+// by the bounds it was given.
+constexpr int kStart = 4;             // blocks that a pair's start and end cost
+constexpr int kLeastShare = 4;
+constexpr int kMostSequences = 1024;  // whose lengths every workgroup adds up
+
+// Length of a pair of sequence b: its blocks (one, which writes the zeros, where it has rows and no tokens) and kStart, or 0.
+// All positions are below 2^31 (cache8_plan).
+__device__ inline int pair_length(const CacheAttnArgs& a, int b) {
+  if (b >= a.c.batch) return 0;
+  int32_t count = 1;
+  if (a.s.offsets != nullptr) {
+    const int32_t lo = a.s.offsets[b], hi = a.s.offsets[b + 1];
+    count = step_range(a.s, lo, hi) ? hi - lo : 0;
+  }
+  const int32_t len = a.c.lens[b];
+  if (count == 0) return 0;
+  return max((len < 0 || len > a.c.max_len ? 0 : len) + kCacheBlock - 1, kCacheBlock) / kCacheBlock + kStart;
+}
+// Sums over the lanes up to each, of 64 numbers >= 0.
+__device__ inline int wave_scan(int x) {
+  // row_shr 1, 2, 4, 8, then the last lane of a row into the next, and that of the first two rows into the others
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+// The pairs' lengths of 64 sequences from b0 on, one a lane, and their sums.
+struct SequenceSums {
+  int mine, upto, all;
+};
+__device__ inline SequenceSums sum_sequences(const CacheAttnArgs& a, int b0) {
+  SequenceSums s;
+  s.mine = pair_length(a, b0 + (int)(threadIdx.x & 63));
+  s.upto = wave_scan(s.mine);
+  s.all = __builtin_amdgcn_readlane(s.upto, 63);
+  return s;
+}
+// Of one head of all sequences; `head`: the sums of the first 64.
+__device__ inline int sum_all(const CacheAttnArgs& a, const SequenceSums& head) {
+  int sum = head.all;
+  for (int b0 = 64; b0 < a.c.batch; b0 += 64) sum += sum_sequences(a, b0).all;
+  return sum;
+}
+__device__ inline int share_of(int all, int shares) {
+  const int each = __builtin_amdgcn_readfirstlane((int)((uint32_t)(all + shares - 1) / (uint32_t)shares));
+  return max((each + 3) & ~3, kLeastShare);  // whole blocks for each of four waves
+}
+// A position in the row of pairs: `in` of the `length` of head lh of sequence b.
+struct ShareAt {
+  int b, lh, in, length;
+};
+// Position x < all.  (No length where there is none: lengths that change while the call runs end it.)
+__device__ inline ShareAt share_at(const CacheAttnArgs& a, const SequenceSums& head, int x) {
+  const int heads = (int)a.heads.d;
+  SequenceSums s = head;
+  int base = 0;
+  for (int b0 = 0; b0 < a.c.batch;) {
+    const uint64_t behind = __builtin_amdgcn_ballot_w64((base + s.upto) * heads > x);
+    if (behind != 0) {
+      const int i = __builtin_ctzll(behind);
+      ShareAt p;
+      p.b = b0 + i;
+      p.length = __builtin_amdgcn_readlane(s.mine, i);
+      const int rest = x - (base + __builtin_amdgcn_readlane(s.upto, i) - p.length) * heads;
+      p.lh = __builtin_amdgcn_readfirstlane((int)((uint32_t)rest / (uint32_t)p.length));
+      p.in = rest - p.lh * p.length;
+      return p;
+    }
+    base += s.all;
+    b0 += 64;
+    s = sum_sequences(a, b0);
+  }
+  return {0, 0, 0, 0};
+}
+// Where workgroup w keeps a row of its part of a pair: it has at most one part with the pair's first block, at its end,
+// and one without it, at its start.
+__device__ inline int64_t share_row(const CacheAttnArgs& a, int w, bool begins, int row) {
+  return (int64_t)(w * 2 + (begins ? 1 : 0)) * (16 * a.tiles) + row;
+}
+
+// The rows of one (sequence, head) pair, or a group of them, on its blocks `first` to `stop` - 1: the outputs, where these are
+// all, or the partial results from row `base` of the workspace on.  NR tiles of 16 rows, W waves.  ONCE: the cache is read
+// once and is not found in a cache by the next call (loads leave it out).
 template <int D, bool FP8, int NR, int W, bool ONCE>
-__global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)) void k_cache8_attention(CacheAttnArgs a) {
+__device__ inline void attend_blocks(const CacheAttnArgs& a, int b, int lh, int group, int first, int stop, int64_t base) {
   using B = Cache8Block<D>;
   constexpr int KS = D / 32;  // products of a score: channels in steps of 32
   constexpr int ND = D / 16;  // output tiles: channels in steps of 16
   constexpr int kStride = D + 4;
   constexpr int kPolicy = ONCE ? 2 : 0;  // nontemporal
-  // Four tiles leave no registers for a block ahead: it waits in LDS, the wave's own keys and, twice, values and scales.
+  // Four tiles leave no registers for a block ahead: it waits in LDS.
   constexpr bool kStaged = NR == 4;
   constexpr int kCodes = 32 * D, kScales = 256, kWaveStage = kStaged ? 2 * kCodes + kScales : 0;
   constexpr int kJoin = 16 * kStride * 4;  // bytes of a wave's outputs of a tile
@@ -78,30 +166,27 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
   __shared__ float2 lds_stat[W][16 * NR];
   const auto lds_o = [&](int w, int row, int x) { return (float*)(lds_wave + w * kWaveLds) + row * kStride + x; };
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int g = lane >> 4, n = lane & 15;
-  const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest);
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));  // nothing that is formed from it is kept from one pair to the next
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, n = lane & 15;
   const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
-  const int chunk = a.by_groups.div(rest), group = a.by_groups.mod(rest, chunk);
-  const int b = blockIdx.y;
-  // 64 of the chunk's pages from page0 on, one a lane
-  int page0 = (chunk * a.chunk / kCacheBlock) >> a.c.page_shift;
+  // 64 of the pair's pages from page0 on, one a lane
+  int page0 = first >> a.c.page_shift;
   const int32_t* row_pages = a.c.table + (int64_t)b * a.c.max_pages;
   const auto load_pages = [&] {
-    const uint32_t at = (uint32_t)(page0 + lane);
-    const int page = (int)at < a.c.max_pages ? *(const int32_t*)((const char*)row_pages + 4 * (uint64_t)at) : -1;
+    const uint32_t i = (uint32_t)(page0 + lane);
+    const int page = (int)i < a.c.max_pages ? *(const int32_t*)((const char*)row_pages + 4 * (uint64_t)i) : -1;
     return page < a.c.num_pages ? page : -1;
   };
   int pages = load_pages();
   const StepSeq q = step_sequence(a.c, a.s, b);
   const RowGroup rg = row_group(a, q, group, 16 * NR);
-  if (rg.row0 >= rg.rows || (chunk > 0 && chunk * a.chunk >= rg.keys)) return;
+  if (rg.row0 >= rg.rows || (first > 0 && first * kCacheBlock >= rg.keys)) return;
 
   uint32_t magic = 0x64646464u;
   asm("" : "+v"(magic));
 
-  const int key0 = chunk * a.chunk, key1 = min(rg.keys, key0 + a.chunk);
-  const int j0 = key0 / kCacheBlock + wave, j1 = (key1 + kCacheBlock - 1) / kCacheBlock;  // every W-th block
+  const int j0 = first + wave, j1 = min(stop, (rg.keys + kCacheBlock - 1) / kCacheBlock);  // every W-th block
   const int all_seen = rg.before + a.R.div(rg.row0) + 1;  // keys before this one are seen by every row of the group
 
   // Block j's part of the lane: keys' bytes and scale, values' bytes and scales, in registers or in LDS.
@@ -432,7 +517,7 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
     __syncthreads();
     // a row's channels by 4 W threads
     constexpr int CH = D / (4 * W);
-    const int row16 = threadIdx.x / (4 * W), c0 = (threadIdx.x % (4 * W)) * CH;
+    const int row16 = (wave * 64 + lane) / (4 * W), c0 = (lane % (4 * W)) * CH;
     const int row = rg.row0 + r * 16 + row16;
     if (row < rg.rows) {
       float2 st = make_float2(kNoMax, 0.0f);
@@ -452,53 +537,170 @@ __global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)
       }
       const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
       const int64_t token = q.row + t;
-      if (rg.keys <= a.chunk) {  // the only chunk
+      if (first == 0 && stop * kCacheBlock >= rg.keys) {
         store_output<CH>(a, layer, token, hq, c0, o, st);
       } else {
-        const int64_t at = partial_row(a, chunk, b, lh, row);
-        if (c0 == 0) a.stat[at] = st;
+        if (c0 == 0) a.stat[base + row] = st;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) a.part[at * D + c0 + i] = o[i];
+        for (int i = 0; i < CH; ++i) a.part[(base + row) * D + c0 + i] = o[i];
       }
     }
   }
+}
+
+// A workgroup a chunk of a pair's tokens and group of its rows.
+template <int D, bool FP8, int NR, int W, bool ONCE>
+__global__ __launch_bounds__(64 * W, (NR == 1 ? 4 : NR == 2 ? 3 : 2) + (D == 64)) void k_cache8_attention(CacheAttnArgs a) {
+  const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest), b = blockIdx.y;
+  const int chunk = a.by_groups.div(rest), group = a.by_groups.mod(rest, chunk), blocks = a.chunk / kCacheBlock;
+  attend_blocks<D, FP8, NR, W, ONCE>(a, b, lh, group, chunk * blocks, (chunk + 1) * blocks, partial_row(a, chunk, b, lh, 0));
+}
+
+// A workgroup a share.
+template <int D, bool FP8, int NR, bool ONCE>
+__global__ __launch_bounds__(256, 2) void k_cache8_shares(CacheAttnArgs a) {
+  const SequenceSums head = sum_sequences(a, 0);
+  const int all = sum_all(a, head) * (int)a.heads.d, share = share_of(all, a.chunks);
+  if ((int64_t)blockIdx.x * share >= all) return;
+  int at = (int)blockIdx.x * share;
+  const int end = (int)min((uint32_t)at + (uint32_t)share, (uint32_t)all);
+  ShareAt pair = share_at(a, head, at);
+  while (pair.length > 0) {
+    const int ends = min(pair.length, pair.in + (end - at)), first = max(pair.in - kStart, 0), stop = ends - kStart;
+    if (stop <= first) return;  // (the share ends before the pair's first block)
+    attend_blocks<D, FP8, NR, 4, ONCE>(a, pair.b, pair.lh, 0, first, stop, share_row(a, (int)blockIdx.x, first == 0, 0));
+    at += ends - pair.in;
+    if (at >= end) return;
+    pair.in = 0;
+    if (++pair.lh == (int)a.heads.d) {
+      pair.lh = 0;
+      do pair.length = __builtin_amdgcn_readfirstlane(pair_length(a, ++pair.b));
+      while (pair.length == 0 && pair.b < a.c.batch);
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the parts of a row whose pair lies in several shares: by a workgroup, whose groups of D / 4 lanes take every
+// kGroups-th part, four channels a lane, each with a reference of its own.
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void k_cache8_join_shares(CacheAttnArgs a) {
+  constexpr int kLanes = D / 4, kGroups = kMergeThreads / kLanes;
+  __shared__ f32x4 lds_o[kGroups][kLanes];
+  __shared__ float2 lds_stat[kGroups];
+  const int row = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, row), b = blockIdx.y;
+  const StepSeq q = step_sequence(a.c, a.s, b);
+  if (row >= q.count * (int)a.R.d) return;
+  // where the pair lies among all
+  SequenceSums s64 = sum_sequences(a, 0);
+  const int heads = (int)a.heads.d, share = share_of(sum_all(a, s64) * heads, a.chunks);
+  int before = 0;
+  for (int b0 = 64; b0 <= b; b0 += 64) {
+    before += s64.all;
+    s64 = sum_sequences(a, b0);
+  }
+  const int length = __builtin_amdgcn_readlane(s64.mine, b & 63);
+  const int from = (before + __builtin_amdgcn_readlane(s64.upto, b & 63) - length) * heads + lh * length;
+  const int w0 = (uint32_t)(from + kStart) / (uint32_t)share, w1 = (uint32_t)(from + length - 1) / (uint32_t)share;
+  if (w0 == w1) return;
+  const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
+  const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
+  const int part = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  float2 st = make_float2(kNoMax, 0.0f);
+  f32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int w = w0 + part; w <= w1; w += kGroups) {
+    const int64_t i = share_row(a, w, w == w0, row);
+    const float2 s = a.stat[i];
+    const f32x4 p = *(const f32x4*)(a.part + i * D + lane * 4);
+    const float top = fmaxf(st.x, s.x);
+    const float f = __builtin_amdgcn_exp2f(st.x - top), fs = __builtin_amdgcn_exp2f(s.x - top);
+    st = make_float2(top, st.y * f + s.y * fs);
+    o = o * f + p * fs;
+  }
+  lds_o[part][lane] = o;
+  if (lane == 0) lds_stat[part] = st;
+  __syncthreads();
+  if (part != 0) return;
+  float top = kNoMax;
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) top = fmaxf(top, lds_stat[i].x);
+  st = make_float2(top, 0.0f);
+  o = (f32x4){0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    const float2 s = lds_stat[i];
+    const float f = __builtin_amdgcn_exp2f(s.x - top);
+    st.y += s.y * f;
+    o += lds_o[i][lane] * f;
+  }
+  const float x[4] = {o.x, o.y, o.z, o.w};
+  store_output<4>(a, layer, q.row + t, hq, lane * 4, x, st);
 }
 
 }  // namespace
 
 constexpr int64_t kStreamed = 256 << 20;  // bytes of a cache that the chip's caches do not hold
 
-// The 4-bit cache's division into rows and chunks, with this cache's bytes.
+// The 4-bit cache's division into rows and chunks, but that decoding calls which it would split are cut into shares on the
+// device (chunk 0), one a CU with one tile of rows, two with two.
 CachePlan cache8_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
                       int32_t max_len) {
+  constexpr int64_t kCus = 256;
   CachePlan p = cache_plan(L, Hq, Hkv, head_dim, batch, max_new, max_len);
-  p.once = p.row_groups == 1 && (double)L * Hkv * batch * max_len * (double)cache8_block_bytes(head_dim) / kCacheBlock >
+  const int64_t heads = (int64_t)L * Hkv * batch, length = ((int64_t)max_len + kCacheBlock - 1) / kCacheBlock + kStart;
+  p.once = p.row_groups == 1 && (double)heads * max_len * (double)cache8_block_bytes(head_dim) / kCacheBlock >
                                     (double)kStreamed;
+  if (p.tiles < 4 && p.chunks > 1 && batch <= kMostSequences && heads * length < (int64_t)1 << 31) {
+    p.chunk = 0;
+    p.chunks = (int32_t)((p.tiles == 1 ? 1 : 2) * kCus);
+  }
+  // A workgroup's two partial results, of 32 rows at most, in the bound of cache_plan, which never falls.
+  if (max_len > 512) {
+    const int64_t rows = 32 * 2 * std::min(2 * kCus, heads * length / kLeastShare + 1);
+    const size_t o_off = ((size_t)rows * sizeof(float2) + 255) / 256 * 256;
+    const size_t total = o_off + (size_t)rows * head_dim * sizeof(float);
+    if (p.chunk == 0) p.o_off = o_off;
+    p.total = std::max(p.total, total);
+  }
   return p;
 }
 
 namespace {
 
 template <int D, bool FP8, int NR, int W>
-void launch_part(const CacheAttnArgs& a, dim3 grid, hipStream_t stream) {
+void launch_chunks(const CacheAttnArgs& a, dim3 grid, hipStream_t stream) {
   if (a.once)
     hipLaunchKernelGGL((k_cache8_attention<D, FP8, NR, W, true>), grid, dim3(64 * W), 0, stream, a);
   else
     hipLaunchKernelGGL((k_cache8_attention<D, FP8, NR, W, false>), grid, dim3(64 * W), 0, stream, a);
 }
 
+template <int D, bool FP8, int NR>
+void launch_shares(const CacheAttnArgs& a, hipStream_t stream) {
+  if (a.once)
+    hipLaunchKernelGGL((k_cache8_shares<D, FP8, NR, true>), dim3(a.chunks), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_cache8_shares<D, FP8, NR, false>), dim3(a.chunks), dim3(256), 0, stream, a);
+}
+
 template <int D, bool FP8>
 hipError_t launch_attention(const CacheAttnArgs& a, hipStream_t stream) {
   const unsigned heads = (unsigned)(a.c.L * a.c.Hkv), batch = (unsigned)a.c.batch;
+  const bool shares = a.chunk == 0;
   const dim3 grid(heads * a.row_groups * a.chunks, batch);
-  if (a.tiles == 1 && a.waves == 8) launch_part<D, FP8, 1, 8>(a, grid, stream);
-  else if (a.tiles == 1) launch_part<D, FP8, 1, 4>(a, grid, stream);
-  else if (a.tiles == 2) launch_part<D, FP8, 2, 4>(a, grid, stream);
-  else launch_part<D, FP8, 4, 4>(a, grid, stream);
+  if (shares && a.tiles == 1) launch_shares<D, FP8, 1>(a, stream);
+  else if (shares) launch_shares<D, FP8, 2>(a, stream);
+  else if (a.tiles == 1 && a.waves == 8) launch_chunks<D, FP8, 1, 8>(a, grid, stream);
+  else if (a.tiles == 1) launch_chunks<D, FP8, 1, 4>(a, grid, stream);
+  else if (a.tiles == 2) launch_chunks<D, FP8, 2, 4>(a, grid, stream);
+  else launch_chunks<D, FP8, 4, 4>(a, grid, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.chunks == 1) return e;
   const unsigned rows = heads * a.row_groups * a.tiles * 16;  // 16 a tile
-  if (a.chunks >= 8)
+  if (shares)
+    hipLaunchKernelGGL((k_cache8_join_shares<D>), dim3(heads * a.R.d * a.s.max_new, batch), dim3(kMergeThreads), 0, stream, a);
+  else if (a.chunks >= 8)
     hipLaunchKernelGGL((k_cache_merge<D, 4>), dim3(rows, batch), dim3(kMergeThreads), 0, stream, a);
   else
     hipLaunchKernelGGL((k_cache_merge<D, 1>), dim3(rows / 4, batch), dim3(kMergeThreads), 0, stream, a);

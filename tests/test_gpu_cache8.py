@@ -560,6 +560,70 @@ def test_attention_of_many_whole_sequences(gpu_lib, d, most, fmt):
 
 
 @by_fmt
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", ["few", "tiny", "mixed", "long", "drafts", "many", "more"])
+def test_attention_in_shares(gpu_lib, case, d, fmt):
+    """Decoding calls whose work is divided on the device: pairs that lie in one workgroup's share, begin or end in it, or span
+    several, sequences without tokens, rows or a range that counts among them, batches of more than 64 sequences, and of
+    more than the division takes."""
+    rng = np.random.default_rng(91)
+    Hq, Hkv, page, only, bound = 4, 2, 64, None, 1 << 19
+    if case == "few":
+        lens, new = [1, 33, 4000], [1, 1, 1]
+    elif case == "tiny":
+        lens, new = [int(n) for n in rng.integers(0, 40, 130)], [1] * 130
+    elif case == "mixed":
+        lens, new = [0, 1500, 17, 0, 0, 2900, 1, 31, 32, 33, 700, 0, 64], [1, 1, 0, 1, 0, 1, 1, 1, 1, 1, 1, 1, 0]
+    elif case == "long":
+        lens, new, Hkv, Hq = [30011, 5], [1, 1], 1, 2
+    elif case == "drafts":
+        lens, new, Hq = [5, 900, 0, 3100, 40, 2, 64], [8, 3, 2, 7, 0, 4, 1], 6  # three query heads a KV head: 24 rows
+    elif case == "many":
+        lens = [int(n) for n in rng.integers(0, 90, 300)]
+        lens[77], lens[201], lens[299] = 2500, 1200, 800
+        new, only = [1] * 300, [0, 1, 63, 64, 76, 77, 78, 128, 200, 201, 202, 298, 299]
+    else:
+        lens = [int(n) for n in rng.integers(0, 20, 1030)]
+        lens[3], lens[1029] = 5000, 4100  # in chunks
+        new, Hkv, Hq, only, bound = [1] * 1030, 1, 1, [0, 3, 4, 500, 1028, 1029], 1 << 16
+    s = Setup(92, fmt, 1, Hq, Hkv, d, page, lens, cols=bound // page)
+    q = s.rows(max(sum(new), 1), Hq)
+    step = B.Step(q.shape[1], max(new), torch.from_numpy(offsets_of(new)).cuda())
+    ws = torch.full((B.tp_cache8_workspace_size(s.dims, s.cache, step, bound),), 0xFF, dtype=torch.uint8, device="cuda")  # NaN
+    assert ws.numel() > 0
+    out, lse = attend(s, q, new, 0.1, max_len=bound, ws=ws)
+    check_attention(s, q, new, out, lse, 0.1, only=only)
+    again, l2 = attend(s, q, new, 0.1, max_len=bound, ws=ws)
+    assert torch.equal(out, again) and torch.equal(lse, l2)
+    # the bound that the sequences need: the same within the tolerance
+    out, lse = attend(s, q, new, 0.1, max_len=max(max(lens), 1))
+    check_attention(s, q, new, out, lse, 0.1, only=only)
+
+
+def test_attention_in_shares_with_bad_ranges(gpu_lib):
+    """Ranges and lengths that do not count have no blocks; the pairs behind them keep their places."""
+    lens = [700, 900, 50, 600, 2000, 64]
+    s = Setup(93, c.INT, 1, 4, 2, 64, 32, lens, cols=1 << 14)
+    s.lens_ = [700, 900, 50, 600, 10 ** 9, 64]  # (10^9 counts as 0)
+    s.upload()
+    off = [0, 2, 99, 2, 4, 5, -1]  # 1: leaves the rows, 2 and 5: fall
+    q = s.rows(6, 4)
+    out = torch.full((6, 4, 64), -7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((4, 6), -7.0, device="cuda")
+    B.tp_cache8_attention(s.dims, s.cache, B.Step(6, 2, torch.tensor(off, dtype=torch.int32, device="cuda")), bf16(q[0]).cuda(), 0.1,
+                          1 << 19, out, lse)
+    out, lse = f64(out), f64(lse)
+    for b, rows in ((0, [0, 1]), (3, [2, 3])):
+        for t, row in enumerate(rows):
+            for hq in range(4):
+                k, v, there = s.held(b, 0, hq // 2, lens[b])
+                bound = cc.bounds(q[0, row, hq], k, v, there & (np.arange(lens[b]) <= lens[b] - 2 + t), 0.1)
+                assert cc.accepts(out[row, hq], lse[hq, row], bound), (b, row, hq)
+    assert not out[4].any() and np.all(lse[:, 4] == -math.inf)
+    assert np.all(out[5] == -7) and np.all(lse[:, 5] == -7)
+
+
+@by_fmt
 def test_attention_strides(gpu_lib, fmt):
     """Queries inside a fused projection's rows, head-major queries and outputs, an output between guards, one query for all."""
     s = Setup(34, fmt, 1, 8, 2, 64, 32, [90, 41])
