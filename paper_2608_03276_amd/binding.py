@@ -6,6 +6,7 @@ machine without the built library raises ImportError (there is no fallback).
 """
 from __future__ import annotations
 
+import array
 import contextlib
 import ctypes
 import os
@@ -84,8 +85,11 @@ class TpRope(ctypes.Structure):
 
 
 def _i64_array(vals):
-    vals = [int(v) for v in vals]
-    return (ctypes.c_int64 * len(vals))(*vals)
+    try:
+        out = array.array("q", vals)
+    except TypeError:  # not whole numbers by type
+        out = array.array("q", [int(v) for v in vals])
+    return (ctypes.c_int64 * len(out)).from_buffer(out)
 
 
 class Batch:

@@ -78,6 +78,48 @@ __device__ inline uint2 widened(uint32_t w) {
   return make_uint2((a ^ 0x08080808u) + 0x78787878u, (b ^ 0x08080808u) + 0x78787878u);
 }
 
+// One token's query rows, kAhead passes of loads in flight.  The loads come first, then what decides whether they count.
+template <int D, int T>
+__device__ inline void rotate_query_rows(const CacheWriteArgs& a, int unit) {
+  constexpr int LPT = D / 8, kHeads = T / LPT, kAhead = D == 128 && T == kRowsThreads ? 4 : 1;
+  const int layer = a.by_total.div(unit), row = a.by_total.mod(unit, layer);
+  const int piece = threadIdx.x % LPT;
+  const bool turn = rotates(a, piece);
+  const int other = turn && !a.pairs ? partner(a, piece) : piece;
+  const uint16_t* from = a.q.data + layer * a.q.layer + row * a.q.token;
+  uint16_t* to = a.q_out.data + layer * a.q_out.layer + row * a.q_out.token;
+  uint4 x[kAhead], y[kAhead];
+  const auto load = [&](int h0) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + i * kHeads + (int)threadIdx.x / LPT;
+      x[i] = y[i] = make_uint4(0, 0, 0, 0);
+      if (h >= a.Hq) continue;
+      x[i] = *((const uint4*)(from + h * a.q.head) + piece);
+      if (!a.pairs) y[i] = *((const uint4*)(from + h * a.q.head) + other);
+    }
+  };
+  load(0);
+  const int64_t pos = scalar_load(a.positions + row);
+  if (pos < 0 || pos >= a.num_positions) return;
+  Angles g = {};
+  if (turn) g = load_angles(a, a.cos_sin + pos * a.rotary_dim, piece);
+  if (a.s.offsets == nullptr ? row >= a.c.batch : !in_a_sequence(a.s, a.c.batch, row)) return;
+  for (int h0 = 0;;) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + i * kHeads + (int)threadIdx.x / LPT;
+      if (h >= a.Hq) break;
+      if (turn) x[i] = rotated(a.pairs, x[i], y[i], g);
+      // (a row's lanes are of one wave and load before they store, so q_out may be q)
+      *((uint4*)(to + h * a.q_out.head) + piece) = x[i];
+    }
+    h0 += kAhead * kHeads;
+    if (h0 >= a.Hq) break;
+    load(h0);
+  }
+}
+
 template <int D, bool FP8, bool LOAD, int T>
 __global__ __launch_bounds__(T) void k_cache8_write(Cache8WriteArgs a, int kv_units) {
   using B = Cache8Block<D>;
@@ -87,7 +129,7 @@ __global__ __launch_bounds__(T) void k_cache8_write(Cache8WriteArgs a, int kv_un
   __shared__ alignas(16) uint8_t codes[kCacheBlock * kStride];
   __shared__ uint32_t tops[T / 64];
   if (!LOAD && (int)blockIdx.x >= kv_units) {
-    rotate_queries<D, T>(a, (int)blockIdx.x - kv_units);
+    rotate_query_rows<D, T>(a, (int)blockIdx.x - kv_units);
     return;
   }
   const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest);

@@ -878,6 +878,90 @@ def test_two_streams(gpu_lib):
         assert torch.equal(out, w[0])
 
 
+@pytest.mark.parametrize("how", ["stream", "handle", "default"])
+def test_scratch_of_the_calls_stream(gpu_lib, monkeypatch, how):
+    """Without a workspace, on a stream that is not the current one: the scratch is that stream's, and the current
+    stream's pending work keeps the memory that it uses."""
+    s = Setup(71, c.FP8, 1, 8, 2, 64, 32, [3000, 500])
+    q = s.rows(2, 8)
+    want, lse = attend(s, q, [1, 1], 0.125)
+    mine, other = torch.cuda.Stream(), torch.cuda.Stream()
+    on = {"stream": other, "handle": other, "default": torch.cuda.default_stream()}[how]
+    given = {"stream": other, "handle": other.cuda_stream, "default": 0}[how]
+    rows, out, l = bf16(q[0]).cuda(), torch.zeros_like(want[0]), torch.zeros_like(lse[0])
+    need = B.tp_cache8_workspace_size(s.dims, s.cache, B.Step(2), 3008)
+    assert need > 0
+    torch.cuda.synchronize()
+    empty, made = torch.empty, []
+
+    def spy(*size, **kw):
+        made.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*size, **kw)
+
+    with torch.cuda.stream(mine):
+        big = torch.ones(64 << 20, device="cuda")
+        held = torch.full((need,), 3, dtype=torch.uint8, device="cuda")
+        kept = held
+        for _ in range(20):
+            big.mul_(1.0)
+        kept = held.clone()  # queued behind the products; the block is free for this stream's next allocation
+        del held
+        monkeypatch.setattr(torch, "empty", spy)
+        B.tp_cache8_attention(s.dims, s.cache, B.Step(2), rows, 0.125, 3008, out, l, stream=given)
+        monkeypatch.undo()
+        assert torch.cuda.current_stream() == mine
+    torch.cuda.synchronize()
+    assert made == [on.cuda_stream]
+    assert torch.equal(out, want[0]) and torch.equal(l, lse[0])
+    assert bool((kept == 3).all())
+
+
+@pytest.mark.parametrize("given", ["current", "stream", "handle"])
+def test_captured_without_a_workspace(gpu_lib, given):
+    """A captured call that makes its own scratch, on the capturing stream: replays against eager calls."""
+    s = Setup(79, c.INT, 1, 8, 2, 64, 32, [3000, 500])
+    side, step = torch.cuda.Stream(), B.Step(2)
+    rows, out = torch.zeros((2, 8, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 8, 64), dtype=torch.bfloat16, device="cuda")
+    stream = {"current": None, "stream": side, "handle": side.cuda_stream}[given]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        B.tp_cache8_attention(s.dims, s.cache, step, rows, 0.125, 3008, out, stream=stream)
+    for i in range(4):
+        q = s.rows(2, 8)
+        rows.copy_(bf16(q[0]))
+        want, _ = attend(s, q, [1, 1], 0.125)
+        other = [torch.full((1 << 20,), i, device="cuda") for _ in range(3)]  # the program's own memory
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0])
+        assert all(bool((x == i).all()) for x in other)
+
+
+def test_captured_step_follows_its_lengths(gpu_lib):
+    """One captured call for lengths from 0 to its bound: every replay is that of the lengths that the tensor holds, also
+    where the division into shares changes."""
+    bound = 1 << 15
+    s = Setup(80, c.FP8, 1, 4, 1, 128, 64, [9000, 700, 3, 5000], cols=bound // 64)
+    q = s.rows(4, 4)
+    rows = bf16(q[0]).cuda()
+    out, lse = torch.zeros((4, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((4, 4), device="cuda")
+    ws = torch.empty(B.tp_cache8_workspace_size(s.dims, s.cache, B.Step(4), bound), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        B.tp_cache8_attention(s.dims, s.cache, B.Step(4), rows, 0.1, bound, out, lse, ws)
+    for lens in ([9000, 700, 3, 5000], [1, 0, 0, 2], [0, 0, 0, 0], [33, 700, 1, 4999], [9000, 0, 3, 1]):
+        s.lens_ = lens
+        s.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        ws.fill_(0xFF)
+        out.fill_(-7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_attention(s, q, [1] * 4, out[None], lse[None], 0.1)
+
+
 def test_formats_do_not_mix(gpu_lib):
     """A handle of one width is refused by the other's calls."""
     s4 = T.Setup(62, 1, 2, 2, 64, 32, [5])
