@@ -581,16 +581,20 @@ __global__ __launch_bounds__(256, 2) void k_cache8_shares(CacheAttnArgs a) {
   }
 }
 
-// Joins the parts of a row whose pair lies in several shares: by a workgroup, whose groups of D / 4 lanes take every
-// kGroups-th part, four channels a lane, each with a reference of its own.
-template <int D>
+// Joins the parts of a row whose pair lies in several shares: by WPR waves, whose groups of D / 4 lanes take every kGroups-th
+// part, four channels a lane, each with a reference of its own.  A workgroup has several rows of a pair.
+template <int D, int WPR>
 __global__ __launch_bounds__(kMergeThreads) void k_cache8_join_shares(CacheAttnArgs a) {
-  constexpr int kLanes = D / 4, kGroups = kMergeThreads / kLanes;
-  __shared__ f32x4 lds_o[kGroups][kLanes];
-  __shared__ float2 lds_stat[kGroups];
-  const int row = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, row), b = blockIdx.y;
+  constexpr int kLanes = D / 4;
+  constexpr int kGroups = WPR * 64 / kLanes;
+  constexpr int kRows = kMergeThreads / 64 / WPR;
+  __shared__ f32x4 lds_o[kRows][kGroups][kLanes];
+  __shared__ float2 lds_stat[kRows][kGroups];
+  const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest), b = blockIdx.y;
+  const int mine = threadIdx.x / (WPR * 64);  // row of the workgroup
+  const int row = rest * kRows + mine;
+  const int part = threadIdx.x % (WPR * 64) / kLanes, lane = threadIdx.x % kLanes;
   const StepSeq q = step_sequence(a.c, a.s, b);
-  if (row >= q.count * (int)a.R.d) return;
   // where the pair lies among all
   SequenceSums s64 = sum_sequences(a, 0);
   const int heads = (int)a.heads.d, share = share_of(sum_all(a, s64) * heads, a.chunks);
@@ -602,38 +606,39 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache8_join_shares(CacheAttnA
   const int length = __builtin_amdgcn_readlane(s64.mine, b & 63);
   const int from = (before + __builtin_amdgcn_readlane(s64.upto, b & 63) - length) * heads + lh * length;
   const int w0 = (uint32_t)(from + kStart) / (uint32_t)share, w1 = (uint32_t)(from + length - 1) / (uint32_t)share;
-  if (w0 == w1) return;
-  const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
-  const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
-  const int part = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const bool in = row < q.count * (int)a.R.d && w0 != w1;
   float2 st = make_float2(kNoMax, 0.0f);
   f32x4 o = {0, 0, 0, 0};
+  if (in) {
 #pragma unroll 4
-  for (int w = w0 + part; w <= w1; w += kGroups) {
-    const int64_t i = share_row(a, w, w == w0, row);
-    const float2 s = a.stat[i];
-    const f32x4 p = *(const f32x4*)(a.part + i * D + lane * 4);
-    const float top = fmaxf(st.x, s.x);
-    const float f = __builtin_amdgcn_exp2f(st.x - top), fs = __builtin_amdgcn_exp2f(s.x - top);
-    st = make_float2(top, st.y * f + s.y * fs);
-    o = o * f + p * fs;
+    for (int w = w0 + part; w <= w1; w += kGroups) {
+      const int64_t i = share_row(a, w, w == w0, row);
+      const float2 s = a.stat[i];
+      const f32x4 p = *(const f32x4*)(a.part + i * D + lane * 4);
+      const float top = fmaxf(st.x, s.x);
+      const float f = __builtin_amdgcn_exp2f(st.x - top), fs = __builtin_amdgcn_exp2f(s.x - top);
+      st = make_float2(top, st.y * f + s.y * fs);
+      o = o * f + p * fs;
+    }
+    lds_o[mine][part][lane] = o;
+    if (lane == 0) lds_stat[mine][part] = st;
   }
-  lds_o[part][lane] = o;
-  if (lane == 0) lds_stat[part] = st;
   __syncthreads();
-  if (part != 0) return;
+  if (!in || part != 0) return;
   float top = kNoMax;
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) top = fmaxf(top, lds_stat[i].x);
+  for (int i = 0; i < kGroups; ++i) top = fmaxf(top, lds_stat[mine][i].x);
   st = make_float2(top, 0.0f);
   o = (f32x4){0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < kGroups; ++i) {
-    const float2 s = lds_stat[i];
+    const float2 s = lds_stat[mine][i];
     const float f = __builtin_amdgcn_exp2f(s.x - top);
     st.y += s.y * f;
-    o += lds_o[i][lane] * f;
+    o += lds_o[mine][i][lane] * f;
   }
+  const int layer = a.by_Hkv.div(lh), head = a.by_Hkv.mod(lh, layer);
+  const int t = a.R.div(row), hq = head * (int)a.R.d + a.R.mod(row, t);
   const float x[4] = {o.x, o.y, o.z, o.w};
   store_output<4>(a, layer, q.row + t, hq, lane * 4, x, st);
 }
@@ -698,8 +703,11 @@ hipError_t launch_attention(const CacheAttnArgs& a, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.chunks == 1) return e;
   const unsigned rows = heads * a.row_groups * a.tiles * 16;  // 16 a tile
-  if (shares)
-    hipLaunchKernelGGL((k_cache8_join_shares<D>), dim3(heads * a.R.d * a.s.max_new, batch), dim3(kMergeThreads), 0, stream, a);
+  const unsigned pair_rows = a.R.d * (unsigned)a.s.max_new;
+  if (shares && (unsigned)a.chunks <= 8 * heads * batch)  // few parts of a pair
+    hipLaunchKernelGGL((k_cache8_join_shares<D, 1>), dim3(heads * ((pair_rows + 3) / 4), batch), dim3(kMergeThreads), 0, stream, a);
+  else if (shares)
+    hipLaunchKernelGGL((k_cache8_join_shares<D, 4>), dim3(heads * pair_rows, batch), dim3(kMergeThreads), 0, stream, a);
   else if (a.chunks >= 8)
     hipLaunchKernelGGL((k_cache_merge<D, 4>), dim3(rows, batch), dim3(kMergeThreads), 0, stream, a);
   else
