@@ -1,15 +1,31 @@
 // Attention over the paged 8-bit cache (tp_cache8_attention): the newest tokens of each sequence, from one (decoding)
 // to a prompt's chunk, against all its tokens.
 //
-// The division of work is the 4-bit cache's (cache_attention.hip): a workgroup takes 16 to 64 query rows of one
-// (sequence, KV head) and one chunk of the context; its four or eight waves take every fourth or eighth block of 32
-// tokens, with the softmax's running reference and sum in one pass, and join through LDS; chunks join in a second
-// kernel.  Both products are on v_mfma_f32_16x16x32_f16 with the cache as the A operand:
+// A row's output is sum_t p_t v_t / sum_t p_t with p_t = exp(softmax_scale q . k_t - m), in one pass with a running
+// reference m and sum.  attend_blocks does that for 16 to 64 query rows of one (sequence, KV head) and a range of its
+// blocks of 32 tokens; its four or eight waves take every fourth or eighth block and join through LDS.  Both products
+// are on v_mfma_f32_16x16x32_f16 with the cache as the A operand:
 //   scores  S^T = C Q^T of the keys' codes, exact in fp16 (integers up to 127; e4m3 numbers, the smallest 2^-9);
 //           the block's key scale goes into the factor that turns a sum into an exponent, one number a block;
 //   output  O^T += C^T P^T of the values' codes, with the values' scales multiplied into the weights P.
 // Codes become fp16 operands in registers: 0x6400 | u is 1024 + u for a byte u = c + 128 (one byte permutation makes
-// two of them, one packed addition takes 1152 off), and an e4m3 pair is one conversion instruction.
+// two of them, one packed addition takes 1152 off), and an e4m3 pair is one conversion instruction.  Queries are exact
+// in fp16 after a power of two of their row's.  Scores, reference, sum and outputs are fp32; the weights times the
+// values' scales are rounded to fp16, 2^-11, below the output's own 2^-8 (bf16 operands would double that).
+//
+// What a workgroup takes:
+//  - decoding and drafted tokens (up to 32 rows) that have to be split: equal shares of all the call's blocks, cut on the
+//    device (k_cache8_shares, k_cache8_join_shares);
+//  - short ones: whole sequences (k_cache8_attention);
+//  - prompts: 64 rows, whole sequences or chunks that the host plans (k_cache8_attention, k_cache_merge).
+//
+// Measured at d = 128, 8 KV heads.  One row tile is bound by HBM: 48 decoding sequences of 5201 to 23457 tokens, 64 query
+// heads, 1.14 GB: 177 us, 6.4 TB/s, and 5 to join (in chunks that the host plans 213 together); two of 200003 and 98305: 95.7
+// and 4.7.  Two tiles: 16 sequences of 1 to 8 drafted tokens against 2208 to 11710: 46, of which HBM needs 38; the start
+// (lengths, pages, queries: dependent loads) and the waves' join take the rest.  Four tiles: chunks of 1024 and 300 tokens,
+// 14001 and 4096 with those before them, 32 query heads: 246 GFLOP in 247 us, 1.0 PFLOP/s; the issue of vector instructions
+// beside the matrix core's bounds them: 271 and 64 products a wave and block, the matrix core 48 % busy (a stream of products
+// leaves a neighbouring wave 40 % of the vector ALU's issue).
 #include <algorithm>
 
 #include "cache8_block.h"
@@ -65,7 +81,16 @@ __device__ inline void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::
 // workgroup.  A share holds several short pairs or a part of a long one; a pair whose blocks lie in several shares has a
 // partial result in each, which k_cache8_join_shares joins.  So what a call costs goes by what its sequences hold and not
 // by the bounds it was given.
-constexpr int kStart = 4;             // blocks that a pair's start and end cost
+//
+// A share is a workgroup of four waves, one a CU.  Two a CU: 48 sequences of 5000 to 24000 tokens, 64 query heads, 229 -> 237 us,
+// one of 131072 52.1 -> 56.1, of 13215 15.8 -> 15.8, drafted tokens unchanged; 320, 384 or 640 workgroups, which do not divide
+// among the CUs, cost 10 to 25 %.  kStart: a share that begins a pair waits for lengths, pages, queries and a first block, one
+// after another, and joins its waves at the end.  With 4, 8, 12, 16, 24, 32 blocks counted for that: 24 sequences of 100
+// to 9000 tokens 58.1, 53.4, 50.2, 47.2, 47.2, 48.5 us; one of 13215 18.0, 16.9, 15.9, 15.8, 15.8, 15.8; four of 6000 18.5,
+// 20.2, 20.4, 20.1, 20.1, 20.0.  Shares of at least kLeastShare blocks, one a wave: one sequence of 2000 tokens with 4, 8, 16: 9.8,
+// 11.9, 12.9 us, of 1024 9.1, 9.6, 12.3.  Above kMostSequences every workgroup's sum over the lengths costs more than shares
+// save (2000 sequences of 4500, one KV head: 430 us, in the plan's chunks 423; 1024 of 5000: 231, 236).
+constexpr int kStart = 16;            // blocks that a pair's start and end cost
 constexpr int kLeastShare = 4;
 constexpr int kMostSequences = 1024;  // whose lengths every workgroup adds up
 
@@ -157,7 +182,9 @@ __device__ inline void attend_blocks(const CacheAttnArgs& a, int b, int lh, int 
   constexpr int ND = D / 16;  // output tiles: channels in steps of 16
   constexpr int kStride = D + 4;
   constexpr int kPolicy = ONCE ? 2 : 0;  // nontemporal
-  // Four tiles leave no registers for a block ahead: it waits in LDS.
+  // Four tiles leave no registers for a block ahead: it waits in LDS.  (In registers they spilled, and each reload waited
+  // for all loads in flight: prompts 345 us, staged 257.  Rings of three blocks: 259; tiles of 32 rows, 32x32x16 products:
+  // 263 to 296.)
   constexpr bool kStaged = NR == 4;
   constexpr int kCodes = 32 * D, kScales = 256, kWaveStage = kStaged ? 2 * kCodes + kScales : 0;
   constexpr int kJoin = 16 * kStride * 4;  // bytes of a wave's outputs of a tile
@@ -346,7 +373,8 @@ __device__ inline void attend_blocks(const CacheAttnArgs& a, int b, int lh, int 
 #pragma unroll
       for (int r = 0; r < NR; ++r) xs[u][r] = (f32x4){0, 0, 0, 0};
     if (kStaged) {
-      // Operands are read and formed a product ahead: the LDS's latency and the conversions pass beside the products.
+      // Operands are read and formed a product ahead: the LDS's latency and the conversions pass beside the products
+      // (257 -> 253 us).
       Frag qn[NR], kn[2];
 #pragma unroll
       for (int r = 0; r < NR; ++r) qn[r] = query(r, 0);
@@ -582,7 +610,9 @@ __global__ __launch_bounds__(256, 2) void k_cache8_shares(CacheAttnArgs a) {
 }
 
 // Joins the parts of a row whose pair lies in several shares: by WPR waves, whose groups of D / 4 lanes take every kGroups-th
-// part, four channels a lane, each with a reference of its own.  A workgroup has several rows of a pair.
+// part, four channels a lane, each with a reference of its own.  A workgroup has several rows of a pair.  A launch and
+// dependent loads (lengths, statistics, parts) bound it: 4.5 to 5 us.  One wave a row for few parts: 16 sequences' drafts 4.85
+// us (four: 5.4), 48 sequences 4.9 (6.5).
 template <int D, int WPR>
 __global__ __launch_bounds__(kMergeThreads) void k_cache8_join_shares(CacheAttnArgs a) {
   constexpr int kLanes = D / 4;
@@ -645,10 +675,13 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache8_join_shares(CacheAttnA
 
 }  // namespace
 
-constexpr int64_t kStreamed = 256 << 20;  // bytes of a cache that the chip's caches do not hold
+// Bytes of a cache that the chip's caches (256 MB) do not hold from one call to the next: its loads are nontemporal.  (1.07 GB of
+// pages read in any order: 6.63 TB/s, 5.98 without.)
+constexpr int64_t kStreamed = 256 << 20;
 
 // The 4-bit cache's division into rows and chunks, but that decoding calls which it would split are cut into shares on the
-// device (chunk 0), one a CU with one tile of rows, two with two.
+// device (chunk 0), one a CU.  Whole sequences stay whole: 32 of 2300 tokens take 25.1 us in
+// eight waves each, in shares 27.8; 64 of 1024 29.2, 35.9; 64 of 20 to 3000 52.3, 47.8.
 CachePlan cache8_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t batch, int32_t max_new,
                       int32_t max_len) {
   constexpr int64_t kCus = 256;
@@ -658,11 +691,11 @@ CachePlan cache8_plan(int32_t L, int32_t Hq, int32_t Hkv, int32_t head_dim, int3
                                     (double)kStreamed;
   if (p.tiles < 4 && p.chunks > 1 && batch <= kMostSequences && heads * length < (int64_t)1 << 31) {
     p.chunk = 0;
-    p.chunks = (int32_t)((p.tiles == 1 ? 1 : 2) * kCus);
+    p.chunks = (int32_t)kCus;
   }
   // A workgroup's two partial results, of 32 rows at most, in the bound of cache_plan, which never falls.
   if (max_len > 512) {
-    const int64_t rows = 32 * 2 * std::min(2 * kCus, heads * length / kLeastShare + 1);
+    const int64_t rows = 32 * 2 * std::min(kCus, heads * length / kLeastShare + 1);
     const size_t o_off = ((size_t)rows * sizeof(float2) + 255) / 256 * 256;
     const size_t total = o_off + (size_t)rows * head_dim * sizeof(float);
     if (p.chunk == 0) p.o_off = o_off;

@@ -7,6 +7,11 @@
 // 1/2 (1 + 1/2 + 1/4 + ...) of a step however often the scale rises, and an e4m3 code keeps its significant bits.)
 // A key's codes are 8 bytes of the block; a value's are single bytes, which go out by way of LDS, 16 bytes a lane,
 // where the whole block is written, and one by one where it is not: nothing else is read or written of it.
+//
+// Measured at d = 128, 8 KV heads.  HBM bounds long calls: an append of 8191 and 5003 tokens with 64 query heads rotated moves
+// 514 MB in 110 us, 4.7 TB/s; a load of 13107 tokens of 32 layers 2.17 GB in 443 to 464, 4.8; reading them back 2.59 GB in 500,
+// 5.2 (a large copy: 5.4).
+// Short ones take their launch and dependent loads (offsets, lengths, page, block's scale): 4.4 to 5.5 us.
 #include "cache8_block.h"
 #include "cache_rotate.h"
 #include "quant_row.h"
@@ -15,8 +20,14 @@ namespace tp {
 namespace {
 
 constexpr int kRowsThreads = 256;
-// Threads of a step's append, and where it is of more than one block a sequence.
-constexpr int kFewThreads = 512, kFewTokens = 32;
+// An append of one token a sequence at d = 128 has a pass of 512 threads a block and rotates a token's queries in one or two:
+// the chain of loads bounds it (64 sequences, 32 heads: 10.8 us, 256 threads 11.2; 64 heads 12.2, 13.6).  With more tokens 256
+// threads take two passes, whose loads are in flight together (4 tokens a sequence: 15.3 -> 13.9 us).
+constexpr int kOneThreads = 512;
+// From this many query heads on (three passes of 256 threads and more) a token's query rows are loaded four passes ahead at
+// d = 128: 13194 tokens of 64 heads in pairs 148 -> 132 us, in halves 158 -> 154; with 16 heads 81 -> 89 and 88 -> 98 (the
+// registers leave fewer blocks in flight); at d = 64, 64 heads 88 -> 98.
+constexpr int kManyHeads = 33;
 
 // Scales between which the corrected quotient below has normal numbers throughout.
 constexpr float kLeastDivisor = 0x1p-70f, kMostDivisor = 0x1p100f;
@@ -79,9 +90,9 @@ __device__ inline uint2 widened(uint32_t w) {
 }
 
 // One token's query rows, kAhead passes of loads in flight.  The loads come first, then what decides whether they count.
-template <int D, int T>
+template <int D, int T, int kAhead>
 __device__ inline void rotate_query_rows(const CacheWriteArgs& a, int unit) {
-  constexpr int LPT = D / 8, kHeads = T / LPT, kAhead = D == 128 && T == kRowsThreads ? 4 : 1;
+  constexpr int LPT = D / 8, kHeads = T / LPT;
   const int layer = a.by_total.div(unit), row = a.by_total.mod(unit, layer);
   const int piece = threadIdx.x % LPT;
   const bool turn = rotates(a, piece);
@@ -120,7 +131,7 @@ __device__ inline void rotate_query_rows(const CacheWriteArgs& a, int unit) {
   }
 }
 
-template <int D, bool FP8, bool LOAD, int T>
+template <int D, bool FP8, bool LOAD, int T, int AHEAD>
 __global__ __launch_bounds__(T) void k_cache8_write(Cache8WriteArgs a, int kv_units) {
   using B = Cache8Block<D>;
   constexpr int LPT = D / 8;                         // lanes of a row
@@ -129,7 +140,7 @@ __global__ __launch_bounds__(T) void k_cache8_write(Cache8WriteArgs a, int kv_un
   __shared__ alignas(16) uint8_t codes[kCacheBlock * kStride];
   __shared__ uint32_t tops[T / 64];
   if (!LOAD && (int)blockIdx.x >= kv_units) {
-    rotate_query_rows<D, T>(a, (int)blockIdx.x - kv_units);
+    rotate_query_rows<D, T, AHEAD>(a, (int)blockIdx.x - kv_units);
     return;
   }
   const int rest = a.heads.div((int)blockIdx.x), lh = a.heads.mod((int)blockIdx.x, rest);
@@ -380,12 +391,12 @@ void set_heads(Args& a) {
   a.by_Hkv = Divisor::of(a.c.Hkv);
 }
 
-template <int D, bool LOAD, int T>
+template <int D, bool LOAD, int T, int AHEAD>
 void launch_write(const Cache8WriteArgs& a, dim3 grid, int units, hipStream_t stream) {
   if (a.fp8)
-    hipLaunchKernelGGL((k_cache8_write<D, true, LOAD, T>), grid, dim3(T), 0, stream, a, units);
+    hipLaunchKernelGGL((k_cache8_write<D, true, LOAD, T, AHEAD>), grid, dim3(T), 0, stream, a, units);
   else
-    hipLaunchKernelGGL((k_cache8_write<D, false, LOAD, T>), grid, dim3(T), 0, stream, a, units);
+    hipLaunchKernelGGL((k_cache8_write<D, false, LOAD, T, AHEAD>), grid, dim3(T), 0, stream, a, units);
 }
 
 }  // namespace
@@ -396,9 +407,10 @@ hipError_t launch_cache8_append(Cache8WriteArgs& a, int head_dim, hipStream_t st
   a.by_blocks = Divisor::of(a.blocks);
   a.by_total = Divisor::of(a.s.total);
   const dim3 grid((unsigned)units + (a.q.data != nullptr ? (unsigned)(a.c.L * a.s.total) : 0u));
-  if (head_dim == 128 && a.s.max_new <= kFewTokens) launch_write<128, false, kFewThreads>(a, grid, units, stream);
-  else if (head_dim == 128) launch_write<128, false, kRowsThreads>(a, grid, units, stream);
-  else launch_write<64, false, kRowsThreads>(a, grid, units, stream);
+  if (head_dim == 64) launch_write<64, false, kRowsThreads, 1>(a, grid, units, stream);
+  else if (a.s.max_new == 1) launch_write<128, false, kOneThreads, 1>(a, grid, units, stream);
+  else if (a.Hq >= kManyHeads) launch_write<128, false, kRowsThreads, 4>(a, grid, units, stream);
+  else launch_write<128, false, kRowsThreads, 1>(a, grid, units, stream);
   return hipGetLastError();
 }
 
@@ -406,8 +418,8 @@ hipError_t launch_cache8_load(Cache8WriteArgs& a, int head_dim, hipStream_t stre
   const int units = a.c.L * a.c.Hkv * a.blocks;
   const dim3 grid((unsigned)units, (unsigned)a.c.batch);
   set_heads(a);
-  if (head_dim == 128) launch_write<128, true, kRowsThreads>(a, grid, units, stream);
-  else launch_write<64, true, kRowsThreads>(a, grid, units, stream);
+  if (head_dim == 128) launch_write<128, true, kRowsThreads, 1>(a, grid, units, stream);
+  else launch_write<64, true, kRowsThreads, 1>(a, grid, units, stream);
   return hipGetLastError();
 }
 
