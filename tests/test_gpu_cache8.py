@@ -134,6 +134,31 @@ def test_append(gpu_lib, case, fmt):
 
 
 @by_fmt
+@pytest.mark.parametrize("style", [0, 1])
+@pytest.mark.parametrize("Hq,Hkv,new", [(33, 3, [1, 1]), (32, 8, [5, 2]), (33, 3, [3, 1]), (48, 8, [2, 33]), (72, 8, [40, 1]), (130, 2, [4, 2])])
+def test_append_many_query_heads(gpu_lib, Hq, Hkv, new, style, fmt):
+    """Query rows of one to nine passes of a workgroup, whole and not, written apart and in place."""
+    lens = [n + 30 for n in new]
+    s = Setup(17, fmt, 1, Hq, Hkv, 128, 32, lens)
+    off, total = offsets_of(new), sum(new) + 1
+    k, v, q = (s.rows(total, h) for h in (Hkv, Hkv, Hq))
+    cs = table_of(200, 96)
+    pos = s.rng.integers(0, 200, total).astype(np.int32)
+    pos[1] = -1 if sum(new) > 2 else pos[1]
+    q_out = torch.full(q.shape, -7.0, dtype=torch.bfloat16, device="cuda")
+    step = B.Step(total, max(new), torch.from_numpy(off).cuda())
+    kw = dict(positions=torch.from_numpy(pos).cuda(), rope=B.Rope(torch.from_numpy(cs).cuda(), 96, style))
+    q_dev = bf16(q).cuda()
+    B.tp_cache8_append(s.dims, s.cache, step, bf16(k).cuda(), bf16(v).cuda(), q=q_dev, q_out=q_out, **kw)
+    want = append_expected(s, lens, new, off, k, v, q, cs, pos, 96, style)
+    s.check_pages()
+    same(f64(q_out), want)
+    s.upload()
+    B.tp_cache8_append(s.dims, s.cache, step, bf16(k).cuda(), bf16(v).cuda(), q=q_dev, q_out=q_dev, **kw)
+    same(f64(q_dev), np.where(want == -7.0, q, want))
+
+
+@by_fmt
 @pytest.mark.parametrize("d,page", [(64, 32), (128, 64)])
 def test_append_raises_scales(gpu_lib, d, page, fmt):
     """Token by token through two blocks, with keys of growing, falling, zero and equal size: the scale rises by powers of
@@ -598,6 +623,20 @@ def test_attention_in_shares(gpu_lib, case, d, fmt):
     # the bound that the sequences need: the same within the tolerance
     out, lse = attend(s, q, new, 0.1, max_len=max(max(lens), 1))
     check_attention(s, q, new, out, lse, 0.1, only=only)
+
+
+@pytest.mark.parametrize("heads", [(2, 1), (8, 4)])
+def test_attention_in_shares_of_many_sequences(gpu_lib, heads):
+    """The most sequences that are divided on the device, most of them short, a long one first, last and beside others."""
+    rng = np.random.default_rng(94)
+    lens = [int(n) for n in rng.integers(0, 70, 1024)]
+    lens[0], lens[511], lens[512], lens[1023] = 3000, 900, 4000, 2000
+    s = Setup(95, c.FP8, 1, *heads, 64, 64, lens, cols=1 << 10)
+    q = s.rows(1024, heads[0])
+    out, lse = attend(s, q, [1] * 1024, 0.1, max_len=1 << 16)
+    check_attention(s, q, [1] * 1024, out, lse, 0.1, only=[0, 1, 2, 510, 511, 512, 513, 700, 1022, 1023])
+    again, l2 = attend(s, q, [1] * 1024, 0.1, max_len=1 << 16)
+    assert torch.equal(out, again) and torch.equal(lse, l2)
 
 
 def test_attention_in_shares_with_bad_ranges(gpu_lib):
