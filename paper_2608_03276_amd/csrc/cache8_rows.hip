@@ -5,11 +5,12 @@
 // beyond the scale that the block has, the scale is raised by the least power of two that holds it and the codes of
 // the earlier tokens are rounded again.  (A power of two: the error of an integer code is then at most the sum
 // 1/2 (1 + 1/2 + 1/4 + ...) of a step however often the scale rises, and an e4m3 code keeps its significant bits.)
-// A key's codes are 8 bytes of the block; a value's are single bytes, which go out by way of LDS, 16 bytes a lane,
-// where the whole block is written, and one by one where it is not: nothing else is read or written of it.
+// A row's 8 codes are 8 bytes of the block's keys and single bytes of its values.  They go out by way of LDS, 16 bytes a
+// lane, where the whole block is written (the keys written from registers: loads 464 us, so 453), and by themselves where
+// it is not: nothing else is read or written of it.
 //
 // Measured at d = 128, 8 KV heads.  HBM bounds long calls: an append of 8191 and 5003 tokens with 64 query heads rotated moves
-// 514 MB in 110 us, 4.7 TB/s; a load of 13107 tokens of 32 layers 2.17 GB in 443 to 464, 4.8; reading them back 2.59 GB in 500,
+// 514 MB in 110 us, 4.7 TB/s; a load of 13107 tokens of 32 layers 2.17 GB in 429 to 453, 4.9; reading them back 2.59 GB in 500,
 // 5.2 (a large copy: 5.4).
 // Short ones take their launch and dependent loads (offsets, lengths, page, block's scale): 4.4 to 5.5 us.
 #include "cache8_block.h"
@@ -28,6 +29,9 @@ constexpr int kOneThreads = 512;
 // d = 128: 13194 tokens of 64 heads in pairs 148 -> 132 us, in halves 158 -> 154; with 16 heads 81 -> 89 and 88 -> 98 (the
 // registers leave fewer blocks in flight); at d = 64, 64 heads 88 -> 98.
 constexpr int kManyHeads = 33;
+
+// In LDS: the 256 bytes of 16 tokens' keys that lanes of the same channels hold, so that channels begin in different banks.
+constexpr int kKeyGroup = 256 + 16;
 
 // Scales between which the corrected quotient below has normal numbers throughout.
 constexpr float kLeastDivisor = 0x1p-70f, kMostDivisor = 0x1p100f;
@@ -138,6 +142,7 @@ __global__ __launch_bounds__(T) void k_cache8_write(Cache8WriteArgs a, int kv_un
   constexpr int kPasses = kCacheBlock * LPT / T;
   constexpr int kStride = D + 8;                     // bytes of a row of value codes in LDS
   __shared__ alignas(16) uint8_t codes[kCacheBlock * kStride];
+  __shared__ alignas(16) uint8_t keys[D / 8 * kKeyGroup];
   __shared__ uint32_t tops[T / 64];
   if (!LOAD && (int)blockIdx.x >= kv_units) {
     rotate_query_rows<D, T, AHEAD>(a, (int)blockIdx.x - kv_units);
@@ -280,7 +285,11 @@ __global__ __launch_bounds__(T) void k_cache8_write(Cache8WriteArgs a, int kv_un
       vc[p] = codes8<FP8>(vx[p], w ? gamma[p] : 1.0f);  // (lanes without a token do not decide the wave's way)
     }
     if (!w) continue;
-    *(uint2*)(blk + B::kKeys + key8_place<D>(slot, piece)) = kc;
+    const int at = key8_place<D>(slot, piece);
+    if (whole)
+      *(uint2*)(keys + (at >> 8) * kKeyGroup + (at & 255)) = kc;
+    else
+      *(uint2*)(blk + B::kKeys + at) = kc;
     if (piece == 0) *((float*)(blk + B::kValueScales) + slot) = gamma[p];
     if (whole) {
       *(uint2*)(codes + slot * kStride + piece * 8) = vc[p];
@@ -301,6 +310,7 @@ __global__ __launch_bounds__(T) void k_cache8_write(Cache8WriteArgs a, int kv_un
       out[e >> 2] |= (uint32_t)codes[token * kStride + x + (e >> 3) * 16] << (8 * (e & 3));
     }
     *((uint4*)(blk + B::kValues) + i) = make_uint4(out[0], out[1], out[2], out[3]);
+    *((uint4*)(blk + B::kKeys) + i) = *(const uint4*)(keys + (i >> 4) * kKeyGroup + (i & 15) * 16);
   }
 }
 
