@@ -136,7 +136,7 @@ __device__ inline int sum_all(const CacheAttnArgs& a, const SequenceSums& head) 
   return sum;
 }
 __device__ inline int share_of(int all, int shares) {
-  const int each = __builtin_amdgcn_readfirstlane((int)((uint32_t)(all + shares - 1) / (uint32_t)shares));
+  const int each = __builtin_amdgcn_readfirstlane((int)(((uint32_t)all + (uint32_t)shares - 1) / (uint32_t)shares));
   return max((each + 3) & ~3, kLeastShare);  // whole blocks for each of four waves
 }
 // A position in the row of pairs: `in` of the `length` of head lh of sequence b.
@@ -675,9 +675,11 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache8_join_shares(CacheAttnA
 
 }  // namespace
 
-// Bytes of a cache that the chip's caches (256 MB) do not hold from one call to the next: its loads are nontemporal.  (1.07 GB of
-// pages read in any order: 6.63 TB/s, 5.98 without.)
-constexpr int64_t kStreamed = 256 << 20;
+// Bytes of a cache (by the call's bounds) from which on its loads are nontemporal: a step's other layers and their weights push
+// it out of the chip's 256 MB before the next call on it.  Found in no cache, with and without: 32 sequences of about 2300 tokens
+// 30.8 us, 33.6; eight of 13000 44.2, 49.9; one of 13215 14.6, 15.8; one of 2000 (4 MB) 10.5, 10.2.  Where one layer is called again
+// and again they cost: those 32 25.9, 25.1; one of 13215 13.0, 12.1.
+constexpr int64_t kStreamed = 16 << 20;
 
 // The 4-bit cache's division into rows and chunks, but that decoding calls which it would split are cut into shares on the
 // device (chunk 0), one a CU.  Whole sequences stay whole: 32 of 2300 tokens take 25.1 us in
