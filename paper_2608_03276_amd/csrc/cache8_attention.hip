@@ -11,7 +11,7 @@
 // Codes become fp16 operands in registers: 0x6400 | u is 1024 + u for a byte u = c + 128 (one byte permutation makes
 // two of them, one packed addition takes 1152 off), and an e4m3 pair is one conversion instruction.  Queries are exact
 // in fp16 after a power of two of their row's.  Scores, reference, sum and outputs are fp32; the weights times the
-// values' scales are rounded to fp16, 2^-11, below the output's own 2^-8 (bf16 operands would double that).
+// values' scales are rounded to fp16, 2^-11, below the output's own 2^-8 (bf16 operands would add as much again).
 //
 // What a workgroup takes:
 //  - decoding and drafted tokens (up to 32 rows) that have to be split: equal shares of all the call's blocks, cut on the
