@@ -23,7 +23,7 @@
 // heads, 1.14 GB: 177 us, 6.4 TB/s, and 5 to join (in chunks that the host plans 213 together); two of 200003 and 98305: 95.7
 // and 4.7.  Two tiles: 16 sequences of 1 to 8 drafted tokens against 2208 to 11710: 46, of which HBM needs 38; the start
 // (lengths, pages, queries: dependent loads) and the waves' join take the rest.  Four tiles: chunks of 1024 and 300 tokens,
-// 14001 and 4096 with those before them, 32 query heads: 246 GFLOP in 247 us, 1.0 PFLOP/s; the issue of vector instructions
+// 14001 and 4096 with those before them, 32 query heads: 246 GFLOP in 247 us (267 on the slowest card), 1.0 PFLOP/s; the issue of vector instructions
 // beside the matrix core's bounds them: 271 and 64 products a wave and block, the matrix core 48 % busy (a stream of products
 // leaves a neighbouring wave 40 % of the vector ALU's issue).
 #include <algorithm>
