@@ -85,6 +85,7 @@ class TpRope(ctypes.Structure):
 
 
 def _i64_array(vals):
+    vals = list(vals)  # (the array module would take bytes as memory, and part of an iterator before it fails)
     try:
         out = array.array("q", vals)
     except TypeError:  # not whole numbers by type
