@@ -527,9 +527,9 @@ tp_status tp_cache_read(const tp_dims* dims, const tp_cache* cache, const tp_bat
  *   key    one fp32 scale for the block of 32 tokens that the token lies in, c = fl32(k / scale) rounded to the nearest
  *          code (ties to even, at most Q; the sign of a zero is kept), from the bf16 key row (rotated, rounded to bf16).
  *          With m the largest magnitude of the keys that a call writes into a block, the block's scale becomes fl32(m / Q)
- *          if it has no tokens before the call's (or its scale is 0, or not a number that a call has written).  Otherwise its
- *          scale is kept if that is >= fl32(m / Q), and if not becomes 2^n times itself, n the least that reaches fl32(m / Q),
- *          and the codes of the tokens before the call's become c 2^-n, rounded to the nearest code.  So a key held is off by
+ *          if it has no tokens before the call's or its scale is not a finite number above 0.  Otherwise its scale is
+ *          kept if that is >= fl32(m / Q), and if not becomes 2^n times itself, n the least that reaches fl32(m / Q), and
+ *          the codes of the tokens before the call's become c 2^-n, rounded to the nearest code.  So a key held is off by
  *          less than a step of its block's scale (integers: 1/2 (1 + 1/2 + 1/4 + ...) of it, however often the scale rises;
  *          e4m3: half a unit of its last place, and 2^-9 of the scale for numbers that became subnormal).
  *   value  Eq. 2: the scale and codes of tp_quantize_v_scales with the cache's qfmt (8 bits).  tp_cache8_load
@@ -564,8 +564,11 @@ tp_status tp_cache8_load(const tp_dims* dims, const tp_cache8* cache, const int6
 /*
  * A step's new tokens into the pages, as tp_cache_append: keys rotated on the way, and with q their query rows rotated
  * beside them.  Reads the scale and, where that rises, the earlier tokens' key codes of the block that the step begins in:
- * these tokens hold keys (were loaded or appended).  A sequence that is cut back (lens lowered) keeps its last block's
- * scale.  Arguments, limits and errors as tp_cache_append.
+ * these tokens hold keys (were loaded or appended).  A finite scale above 0 counts as theirs, whoever left it there: where a
+ * block's first tokens were never written (skipped for their positions, or a length raised without a call) it is what the
+ * page's memory held, in which later keys may lose all their bits, so a program that does that sets such blocks' scales to 0
+ * first.  A token of the step that is skipped for its position keeps its bytes, but not its key: the block's scale may change.
+ * A sequence that is cut back (lens lowered) keeps its last block's scale.  Arguments, limits and errors as tp_cache_append.
  */
 tp_status tp_cache8_append(const tp_dims* dims, const tp_cache8* cache, const tp_step* step, const tp_rows* k,
                            const tp_rows* v, const int32_t* positions, const tp_rope* rope, const tp_rows* q,

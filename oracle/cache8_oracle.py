@@ -70,7 +70,7 @@ def write_keys(block, d, fmt, before, keys):
     want = np.float32(m / qmax(fmt))
     held = key_scale(block, d) if before > 0 else np.float32(0)
     scale = want
-    if held > 0:
+    if 0 < held < np.inf:
         n = 0
         while float(held) * 2.0 ** n < float(want):
             n += 1

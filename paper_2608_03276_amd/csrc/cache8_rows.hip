@@ -257,11 +257,11 @@ __global__ __launch_bounds__(T) void k_cache8_write(Cache8WriteArgs a, int kv_un
 #pragma unroll
   for (int i = 0; i < T / 64; ++i) top = max(top, tops[i]);
 
-  // the block's scale
+  // the block's scale (one of 0, below it, infinite or NaN is none)
   const float want = __uint_as_float(top << 16) / (FP8 ? 448.0f : 127.0f);
   int up = 0;
   float scale = want;
-  if (held > 0.0f) {
+  if (held > 0.0f && held < INFINITY) {
     if (want > held)
       up = __builtin_amdgcn_frexp_expf(want) - __builtin_amdgcn_frexp_expf(held) +
            (__builtin_amdgcn_frexp_mantf(want) > __builtin_amdgcn_frexp_mantf(held) ? 1 : 0);

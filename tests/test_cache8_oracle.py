@@ -95,6 +95,17 @@ def test_no_scale_and_strange_scales():
 
 
 @pytest.mark.parametrize("fmt", [c.INT, c.FP8])
+@pytest.mark.parametrize("held", [np.inf, -np.inf])
+def test_an_infinite_scale_is_none(held, fmt):
+    d = 64
+    block = np.full(c.block_bytes(d), 0x48, dtype=np.uint8)
+    block[64 * d + 128:64 * d + 132] = np.array([held], dtype=np.float32).view(np.uint8)
+    c.write_keys(block, d, fmt, 2, {2: np.full(d, 1.25)})
+    assert c.key_scale(block, d) == np.float32(1.25 / c.qmax(fmt))
+    assert np.all(block[c.places(d)[0][0]] == 0x48) and np.all(c.codes_of(block[c.places(d)[0][2]], fmt) == c.qmax(fmt))
+
+
+@pytest.mark.parametrize("fmt", [c.INT, c.FP8])
 def test_values_are_the_quantisers(fmt):
     rng = np.random.default_rng(8)
     v = c4.to_bf16(rng.standard_t(3, size=(50, 128)))

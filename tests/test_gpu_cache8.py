@@ -195,6 +195,33 @@ def test_append_raises_scales(gpu_lib, d, page, fmt):
 
 
 @by_fmt
+@pytest.mark.parametrize("d,new", [(64, 1), (128, 1), (128, 3), (64, 40)])
+def test_append_beside_scales_of_any_kind(gpu_lib, d, new, fmt):
+    """Blocks with earlier tokens and a scale that is none (0, negative, NaN, infinite): the keys get one of their own.  A
+    positive finite one, whoever left it, is the block's, however large or small."""
+    none, some = [0.0, -0.0, -1.0, -1e30, math.nan, -math.nan, math.inf, -math.inf], [1e-30, 1e-42, 0.01, 1e30, 3e38]
+    held = np.array(none + some, dtype=np.float32)
+    s = Setup(18, fmt, 1, 2, 2, d, 64, [5 + new] * len(held))
+    for b, x in enumerate(held):
+        at = c4.place_of(s.table[b], s.num, s.page, 0)
+        s.pages[0, at[0], :, at[1], 64 * d + 128:64 * d + 132] = np.array([x]).view(np.uint8)
+    s.upload()
+    off, total = offsets_of([new] * len(held)), new * len(held)
+    k, v = s.rows(total, 2), s.rows(total, 2)
+    B.tp_cache8_append(s.dims, s.cache, B.Step(total, new, torch.from_numpy(off).cuda()), bf16(k).cuda(), bf16(v).cuda())
+    append_expected(s, s.lens_, [new] * len(held), off, k, v, np.zeros((1, total, 2, d)), None, None, 0, 0)
+    s.check_pages()
+    first = min(new, 27)  # the new tokens in the sequences' first blocks
+    for b in range(len(none)):
+        for h in range(2):
+            rows = k[0, off[b]:off[b] + first, h]
+            scale, got = np.float32(np.abs(rows).max() / c.qmax(fmt)), s.held(b, 0, h, 5 + first)[0][5:]
+            # half a step, or half of e4m3's last place of a normal or subnormal code; 2^-23 for the scale and the quotient
+            most = scale / 2 if fmt == c.INT else np.maximum(np.abs(rows) * 2.0 ** -4, scale * 2.0 ** -10)
+            assert np.all(np.abs(got - rows) <= most * (1 + 2.0 ** -10) + np.abs(rows) * 2.0 ** -22), (b, h)
+
+
+@by_fmt
 @pytest.mark.parametrize("power", [-141, -133, -126, -110, -70, -60, 0, 60, 100, 120])
 @pytest.mark.parametrize("d", [64, 128])
 def test_append_odd_values(gpu_lib, d, power, fmt):
