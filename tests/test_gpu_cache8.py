@@ -666,6 +666,42 @@ def test_attention_in_shares_of_many_sequences(gpu_lib, heads):
     assert torch.equal(out, again) and torch.equal(lse, l2)
 
 
+@by_fmt
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", ["tokens", "drafts", "prompts"])
+def test_attention_of_several_layers_split(gpu_lib, case, d, fmt):
+    """Several layers in a call that is divided (one and two tiles of rows) or planned in chunks (four): a pair over many
+    shares, several pairs in one, sequences without tokens; queries and outputs with the layers inside a token's rows."""
+    L, Hkv, bound = 3, 2, 1 << 16
+    lens = [30011, 0, 700] + [(7 * i) % 40 for i in range(40)] + [2100]
+    only = [0, 1, 2, 3, 20, 42, 43]
+    if case == "tokens":
+        Hq, new = 4, [1] * 44
+    elif case == "drafts":
+        Hq, new = 6, [3, 1, 8] + [1 + i % 5 for i in range(40)] + [2]  # up to 24 rows
+    else:
+        L, lens, only, Hq, new, bound = 2, [9000, 40, 700], None, 16, [9, 1, 4], 1 << 14  # up to 72
+    s = Setup(96, fmt, L, Hq, Hkv, d, 64, lens, cols=bound // 64)
+    total = sum(new) + 1
+    q = s.rows(total, Hq)
+    out, lse = attend(s, q, new, 0.1, max_len=bound)
+    check_attention(s, q, new, out, lse, 0.1, only=only)
+    assert bool((out[:, -1] == -7).all()) and bool((lse[:, :, -1] == -7).all())
+    step = B.Step(total, max(new), torch.from_numpy(offsets_of(new)).cuda())
+    inside = bf16(q).cuda().transpose(0, 1).contiguous()  # [total][L][Hq][d]
+    got, l2 = torch.full_like(inside, -7.0), torch.full_like(lse, -7.0)
+    B.tp_cache8_attention(s.dims, s.cache, step, inside.transpose(0, 1), 0.1, bound, got.transpose(0, 1), l2)
+    assert torch.equal(got.transpose(0, 1), out) and torch.equal(l2, lse)
+    for l in range(L):  # a call for each layer alone, on its part of the pages
+        dims = B.dims(1, Hq, Hkv, d)
+        one = B.Cache8(dims, s.dev[l], s.dtable, s.lens, 64, fmt)
+        alone, l1 = torch.full_like(out[l], -7.0), torch.full_like(lse[l], -7.0)
+        B.tp_cache8_attention(dims, one, step, bf16(q[l]).cuda(), 0.1, bound, alone, l1)
+        s1 = Setup.__new__(Setup)
+        s1.__dict__.update(s.__dict__, L=1, pages=s.pages[l:l + 1])
+        check_attention(s1, q[l:l + 1], new, alone[None], l1[None], 0.1, only=[0, 2])
+
+
 def test_attention_in_shares_with_bad_ranges(gpu_lib):
     """Ranges and lengths that do not count have no blocks; the pairs behind them keep their places."""
     lens = [700, 900, 50, 600, 2000, 64]
