@@ -19,13 +19,13 @@
 //  - short ones: whole sequences (k_cache8_attention);
 //  - prompts: 64 rows, whole sequences or chunks that the host plans (k_cache8_attention, k_cache_merge).
 //
-// Measured at d = 128, 8 KV heads.  One row tile is bound by HBM: 48 decoding sequences of 5201 to 23457 tokens, 64 query
-// heads, 1.14 GB: 177 us, 6.4 TB/s, and 5 to join (in chunks that the host plans 213 together); two of 200003 and 98305: 95.7
-// and 4.7.  Two tiles: 16 sequences of 1 to 8 drafted tokens against 2208 to 11710: 46, of which HBM needs 38; the start
-// (lengths, pages, queries: dependent loads) and the waves' join take the rest.  Four tiles: chunks of 1024 and 300 tokens,
-// 14001 and 4096 with those before them, 32 query heads: 246 GFLOP in 247 us (267 on the slowest card), 1.0 PFLOP/s; the issue of vector instructions
-// beside the matrix core's bounds them: 271 and 64 products a wave and block, the matrix core 48 % busy (a stream of products
-// leaves a neighbouring wave 40 % of the vector ALU's issue).
+// Measured at d = 128, 8 KV heads, kernels alone (a bare nontemporal read reaches 7.1 TB/s on this card).  One row tile is bound by
+// HBM: 48 decoding sequences of 5201 to 23457 tokens, 64 query heads, 1.14 GB: 174 us, 6.5 TB/s, and 5 to join (in chunks that the
+// host plans 213 together); two of 200003 and 98305: 93 and 5.  Two tiles: 16 sequences of 1 to 8 drafted tokens against 2208 to
+// 11710: 46, of which HBM needs 33; the start (lengths, pages, queries: dependent loads) and the waves' join take the rest.
+// Four tiles: chunks of 1024 and 300 tokens, 14001 and 4096 with those before them, 32 query heads: 246 GFLOP in 246 to 267 us by
+// the card, 0.92 to 1.0 PFLOP/s; the issue of vector instructions beside the matrix core's bounds them: 271 and 64 products a wave and
+// block, the matrix core 48 % busy (a stream of products leaves a neighbouring wave 40 % of the vector ALU's issue).
 #include <algorithm>
 
 #include "cache8_block.h"
@@ -82,13 +82,14 @@ __device__ inline void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::
 // partial result in each, which k_cache8_join_shares joins.  So what a call costs goes by what its sequences hold and not
 // by the bounds it was given.
 //
-// A share is a workgroup of four waves, one a CU.  Two a CU: 48 sequences of 5000 to 24000 tokens, 64 query heads, 229 -> 237 us,
-// one of 131072 52.1 -> 56.1, of 13215 15.8 -> 15.8, drafted tokens unchanged; 320, 384 or 640 workgroups, which do not divide
+// Times here are of both kernels, each call on a cache that the last ones did not read.  A share is a workgroup of four waves, one a
+// CU.  Two a CU: 48 sequences of 5000 to 24000 tokens, 64 query heads, 1.32 GB, 210 -> 216 us, the 1.14 GB above 183 -> 190, one
+// sequence of 131072 52.1 -> 55.9, of 13215 14.5 -> 15.3, drafted tokens unchanged; 320, 384 or 640 workgroups, which do not divide
 // among the CUs, cost 10 to 25 %.  kStart: a share that begins a pair waits for lengths, pages, queries and a first block, one
-// after another, and joins its waves at the end.  With 4, 8, 12, 16, 24, 32 blocks counted for that: 24 sequences of 100
-// to 9000 tokens 58.1, 53.4, 50.2, 47.2, 47.2, 48.5 us; one of 13215 18.0, 16.9, 15.9, 15.8, 15.8, 15.8; four of 6000 18.5,
-// 20.2, 20.4, 20.1, 20.1, 20.0.  Shares of at least kLeastShare blocks, one a wave: one sequence of 2000 tokens with 4, 8, 16: 9.8,
-// 11.9, 12.9 us, of 1024 9.1, 9.6, 12.3.  Above kMostSequences every workgroup's sum over the lengths costs more than shares
+// after another, and joins its waves at the end.  With 4, 8, 12, 16, 24, 32 blocks counted for that (before loads were
+// nontemporal from 16 MB on): 24 sequences of 100 to 9000 tokens 58.1, 53.4, 50.2, 47.2, 47.2, 48.5 us; one of 13215 18.0, 16.9,
+// 15.9, 15.8, 15.8, 15.8; four of 6000 18.5, 20.2, 20.4, 20.1, 20.1, 20.0.  Shares of at least kLeastShare blocks, one a wave: one
+// sequence of 2000 tokens with 4, 8, 16: 9.8, 11.9, 12.9 us, of 1024 9.1, 9.6, 12.3.  Above kMostSequences every workgroup's sum over the lengths costs more than shares
 // save (2000 sequences of 4500, one KV head: 430 us, in the plan's chunks 423; 1024 of 5000: 231, 236).
 constexpr int kStart = 16;            // blocks that a pair's start and end cost
 constexpr int kLeastShare = 4;
@@ -678,7 +679,9 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache8_join_shares(CacheAttnA
 // Bytes of a cache (by the call's bounds) from which on its loads are nontemporal: a step's other layers and their weights push
 // it out of the chip's 256 MB before the next call on it.  Found in no cache, with and without: 32 sequences of about 2300 tokens
 // 30.8 us, 33.6; eight of 13000 44.2, 49.9; one of 13215 14.6, 15.8; one of 2000 (4 MB) 10.5, 10.2.  Where one layer is called again
-// and again they cost: those 32 25.9, 25.1; one of 13215 13.0, 12.1.
+// and again, or a model's layers and weights stay below that together, they mostly cost: 32 of 300 (20 MB) 8.5, 7.3; one of 13107
+// 14.0, 12.7; 32 of 2300 26.3, 25.3; 48 of 2000 (200 MB) 38.1, 32.4, the most seen; one of 40000 19.6, 20.6.  A call whose bound is
+// far above what its sequences hold is streamed too (eight of 1000 with a bound of 131072: 12.0 either way).
 constexpr int64_t kStreamed = 16 << 20;
 
 // The 4-bit cache's division into rows and chunks, but that decoding calls which it would split are cut into shares on the

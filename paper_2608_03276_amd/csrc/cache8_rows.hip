@@ -11,7 +11,7 @@
 //
 // Measured at d = 128, 8 KV heads.  HBM bounds long calls: an append of 8191 and 5003 tokens with 64 query heads rotated moves
 // 514 MB in 110 us, 4.7 TB/s; a load of 13107 tokens of 32 layers 2.17 GB in 429 to 453, 4.9; reading them back 2.59 GB in 500,
-// 5.2 (a large copy: 5.4).
+// 5.2 (a plain large copy 5.3 to 5.5, one with nontemporal loads and stores 6.2).
 // Short ones take their launch and dependent loads (offsets, lengths, page, block's scale): 4.4 to 5.5 us.
 #include "cache8_block.h"
 #include "cache_rotate.h"
@@ -27,7 +27,8 @@ constexpr int kRowsThreads = 256;
 constexpr int kOneThreads = 512;
 // From this many query heads on (three passes of 256 threads and more) a token's query rows are loaded four passes ahead at
 // d = 128: 13194 tokens of 64 heads in pairs 148 -> 132 us, in halves 158 -> 154; with 16 heads 81 -> 89 and 88 -> 98 (the
-// registers leave fewer blocks in flight); at d = 64, 64 heads 88 -> 98.
+// registers leave fewer blocks in flight); at d = 64, 64 heads 88 -> 98.  Few tokens lose by it (two each of 64 sequences, 64
+// heads: 15.2 -> 16.7), which the rule does not look at.
 constexpr int kManyHeads = 33;
 
 // In LDS: the 256 bytes of 16 tokens' keys that lanes of the same channels hold, so that channels begin in different banks.
