@@ -216,9 +216,9 @@ def test_append_beside_scales_of_any_kind(gpu_lib, d, new, fmt):
         for h in range(2):
             rows = k[0, off[b]:off[b] + first, h]
             scale, got = np.float32(np.abs(rows).max() / c.qmax(fmt)), s.held(b, 0, h, 5 + first)[0][5:]
-            # half a step, or half of e4m3's last place of a normal or subnormal code; 2^-23 for the scale and the quotient
+            # half a step, or half of e4m3's last place of a normal or subnormal code; 2^-24 each for scale and quotient
             most = scale / 2 if fmt == c.INT else np.maximum(np.abs(rows) * 2.0 ** -4, scale * 2.0 ** -10)
-            assert np.all(np.abs(got - rows) <= most * (1 + 2.0 ** -10) + np.abs(rows) * 2.0 ** -22), (b, h)
+            assert np.all(np.abs(got - rows) <= most + np.abs(rows) * 2.0 ** -23), (b, h)
 
 
 @by_fmt
